@@ -228,7 +228,7 @@ def prepare(case, seed):
 def _norm(s):
     x = s["x"].float() + s["r"].float() if s["r"] is not None else s["x"].float()
     y = x * torch.rsqrt(x.square().mean(1, keepdim=True) + EPS) * s["w"]
-    y = _values(*_quantise(y, 1), 1).bfloat16()  # four bits' values: exact
+    y = _values(*_quantise(y, 1), 1).bfloat16()  # e4m3 values: exact
     return (y, x.to(s["x"].dtype)) if s["r"] is not None else y
 
 
@@ -257,15 +257,17 @@ def _append_one(x, pages, scales, table, pos, count, transposed):
     new = ((src >= 0) & (src < count[:, None, None]))[:, :, None, :, None]
     r = torch.arange(R, device=x.device)[:, None, None]
     fresh = x.float()[r, src.clamp(0, T - 1)].view(R, n, PAGE, H, dh).transpose(2, 3)
-    codes = pages.view(torch.uint8)[ids].view(torch.float8_e4m3fn).float()
-    codes = codes.transpose(3, 4) if transposed else codes
+    was = pages.view(torch.uint8)[ids]
+    was = was.transpose(3, 4) if transposed else was    # [R][n][H][64][dh]
+    codes = was.contiguous().view(torch.float8_e4m3fn).float()
     e = scales.view(torch.uint8)[ids].int()             # [R][n][H]
     zero = torch.zeros((), device=x.device)
     fresh = torch.where(new, fresh, zero)
     kept = torch.where(old, codes * _scale(e)[..., None, None], zero)
     e = torch.where(old.any(3)[..., 0], e, 0).maximum(_exponent(fresh.abs().amax(dim=(3, 4))))
     q = ((kept + fresh) * _scale(254 - e)[..., None, None]).to(torch.float8_e4m3fn)
-    q = (q.transpose(3, 4) if transposed else q).contiguous().view(torch.uint8)
+    q = torch.where(old | new, q.view(torch.uint8), was)  # behind the last token: as it was
+    q = q.transpose(3, 4) if transposed else q
     pages.view(torch.uint8)[ids[used]] = q[used]
     scales.view(torch.uint8)[ids[used]] = e.to(torch.uint8)[used]
 
@@ -408,7 +410,7 @@ def _append64(x, pages, scales, table, pos, count, transposed):
             s = torch.exp2(e)
             if lo > PAGE * p:
                 s = torch.maximum(s, scales[i])
-            body = torch.zeros_like(old)
+            body = old.clone()
             body[:, :lo - PAGE * p] = _e4m3(old[:, :lo - PAGE * p] * (scales[i] / s)[:, None, None])
             body[:, lo - PAGE * p:hi - PAGE * p] = _e4m3(new / s[:, None, None])
             pages[i] = body.transpose(1, 2) if transposed else body
