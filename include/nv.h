@@ -40,7 +40,7 @@ typedef enum {
   NV_ERR_WORKSPACE = -5      /* workspace pointer null or smaller than required */
 } nv_status;
 
-typedef enum { NV_F32 = 0, NV_BF16 = 1 } nv_dtype;
+typedef enum { NV_F32 = 0, NV_BF16 = 1, NV_F16 = 2 } nv_dtype;
 
 /* Text for a status code.  Never NULL. */
 const char* nv_status_string(int32_t status);
@@ -494,6 +494,113 @@ int32_t nv_op_conv3x3(const void* x, const void* x2, const void* w, const float*
 int32_t nv_op_attention(const void* q, const void* k, const void* vt, void* out, int32_t rows,
                         int32_t S, int32_t L, int32_t heads, int32_t dh, int32_t ldq, int32_t ldk,
                         int32_t ldo, int64_t vt_ld, int64_t vt_row, float scale, void* stream);
+
+/* ------------------------------------------------------------------------ *
+ * The 8-bit path: what a transformer layer needs to run on the e4m3 matrix
+ * cores and to keep its keys and values in 8 bits.  It stands beside the
+ * float16 layers above; outputs are float16 or bfloat16 (dtype NV_F16 or
+ * NV_BF16; NV_F32 only where said).
+ *
+ * 8-bit form of a matrix: e4m3 codes (OCP "fn": largest 448, one NaN, no
+ * infinities) in rows that start ldq bytes apart, and one scale byte e for
+ * each block, of value 2^(e - 127) (255: NaN): an element is code * 2^(e - 127).
+ * A block is 128 consecutive columns of one row (block_rows 1: activations,
+ * scales [M][ceil(K / 128)]) or of 128 rows (block_rows 128: weights, scales
+ * [ceil(M / 128)][ceil(K / 128)]); the last blocks may be short.  The scale
+ * the library writes is the smallest with amax <= 448 * 2^(e - 127), at least
+ * e = 1, amax over the block's finite elements; codes are rounded to nearest
+ * even, and elements that are not finite become NaN.
+ *
+ * Sizes of zero (M, rows, S, T) are legal and launch nothing.  Strides are in
+ * elements (bytes for 8-bit rows).  Buffers that are not 16-byte aligned, or
+ * rows whose stride or length does not keep 8 elements together, are taken
+ * element by element (nv_op_linear8's operands: refused, see there).  Inputs
+ * and outputs may not overlap unless said.
+ *
+ * nv_op_quant8: x [M] rows of K (x_dtype NV_F32, NV_F16 or NV_BF16, ldx apart)
+ *   into 8-bit form.  1 <= K.
+ * nv_op_dequant8: the values of an 8-bit matrix in out_dtype (NV_F32, NV_F16,
+ *   NV_BF16): float32 and bfloat16 hold every value exactly (but for results
+ *   below 2^-126), float16 rounds and overflows to infinity.
+ * nv_op_rmsnorm8: s = x + residual (NULL: x) in float32,
+ *   y = s * weight / sqrt(mean(s^2) + eps) in float32 from that sum, written in
+ *   8-bit form with block_rows 1; h (NULL: not written) receives s rounded to
+ *   dtype (NV_F16 or NV_BF16), the residual stream of the next layer; h may be
+ *   x or residual itself with the same stride.  1 <= D <= 32768 (beyond:
+ *   NV_ERR_UNSUPPORTED); weight device f32 [D]; eps >= 0 and finite.
+ * ------------------------------------------------------------------------ */
+int32_t nv_op_quant8(const void* x, int32_t x_dtype, int64_t ldx, int64_t M, int32_t K,
+                     int32_t block_rows, void* q, int64_t ldq, uint8_t* scales, void* stream);
+int32_t nv_op_dequant8(const void* q, int64_t ldq, const uint8_t* scales, int64_t M, int32_t K,
+                       int32_t block_rows, void* out, int32_t out_dtype, int64_t ldo,
+                       void* stream);
+int32_t nv_op_rmsnorm8(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                       int32_t dtype, const float* weight, float eps, int64_t M, int32_t D,
+                       void* h, int64_t ldh, void* q, int64_t ldq, uint8_t* scales,
+                       void* stream);
+
+/* nv_op_linear8: out[m][n] = sum_k x[m][k] w[n][k] (+ bias[n]) (+ residual[m][n])
+ *   over the values of the 8-bit matrices x [M][K] (block_rows 1, scales xs) and
+ *   w [N][K] (block_rows 128, scales ws), float32 accumulation, one rounding to
+ *   dtype (NV_F16 or NV_BF16).  x and w 16-byte aligned, ldx and ldw multiples
+ *   of 16 and >= K (NV_ERR_UNSUPPORTED otherwise); K any: the bytes of a row
+ *   behind K may hold anything.  bias device f32 [N] or NULL; residual in
+ *   dtype, ldr apart, or NULL; it may be out itself with the same stride.
+ *   M <= 2^31 - 1.  workspace: device, >= nv_op_linear8_workspace(M, N, K)
+ *   bytes (0: may be NULL), 256-byte aligned, contents need not be
+ *   initialised. */
+size_t nv_op_linear8_workspace(int64_t M, int32_t N, int32_t K);
+int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void* w, int64_t ldw,
+                      const uint8_t* ws, const float* bias, const void* residual, int64_t ldr,
+                      void* out, int64_t ldo, int32_t dtype, int64_t M, int32_t N, int32_t K,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Keys and values kept in 8 bits.  A page holds NV_KV8_PAGE = 64 consecutive
+ * tokens of one sequence: kp [n_pages][heads][64][dh] and vp
+ * [n_pages][heads][dh][64] (values transposed, as nv_op_attention takes them)
+ * hold e4m3 codes, ks and vs [n_pages][heads] the scale byte of each page and
+ * head.  table (device int32 [rows][table_w]) names the page of tokens
+ * 64 j .. 64 j + 63 of each row; an entry outside [0, n_pages) is a hole: its
+ * tokens are not stored and not seen.  dh in {16, 32, 40, 64, 80, 128, 160};
+ * kp and vp 16-byte aligned.
+ *
+ * nv_op_kv8_append: the first count[r] (device int32 [rows], clamped to
+ *   [0, T]; NULL: all T) tokens of row r of k and v (in dtype NV_F16 or NV_BF16;
+ *   token t of row r, head h at r * row_stride + t * ld + h * dh) become tokens
+ *   pos[r] .. (device int32 [rows], >= 0; a negative one stores nothing) of its
+ *   sequence.  A page that takes its first token starts a new scale; one that
+ *   holds tokens before pos[r] keeps its scale unless a new token needs a larger
+ *   one, and then its old codes are rounded to that.  Codes of tokens behind the
+ *   last one stay as they were; tokens past the table's end are dropped.  A page
+ *   that is written may be named once among all rows.
+ *
+ * nv_op_attention_kv8: o[i] = sum_j softmax_j(scale q[i] . k_j) v_j over the
+ *   tokens j < lens[r] (device int32 [rows], clamped to the table's tokens) of
+ *   row r that are in no hole and, with qpos (device int32 [rows]; NULL: no
+ *   limit), j <= qpos[r] + i.  q and out in dtype: query i of row r, head h at
+ *   r * row_stride + i * ld + h * dh (strides in multiples of 8, 16-byte
+ *   aligned: NV_ERR_UNSUPPORTED otherwise).  heads a multiple of kv_heads:
+ *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
+ *   token gets zeros.  Codes and scales of tokens that no query sees may hold
+ *   anything, NaN among it.  float32 scores, softmax and sums; the
+ *   probabilities enter the second product in dtype.  scale finite.
+ *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be
+ *   NULL), 256-byte aligned, contents need not be initialised. */
+#define NV_KV8_PAGE 64
+int32_t nv_op_kv8_append(const void* k, int64_t ldk, int64_t k_row_stride, const void* v,
+                         int64_t ldv, int64_t v_row_stride, int32_t dtype, int32_t rows,
+                         int32_t T, int32_t heads, int32_t dh, void* kp, void* vp, uint8_t* ks,
+                         uint8_t* vs, int64_t n_pages, const int32_t* table, int32_t table_w,
+                         const int32_t* pos, const int32_t* count, void* stream);
+size_t nv_op_attention_kv8_workspace(int32_t rows, int32_t S, int32_t heads, int32_t kv_heads,
+                                     int32_t dh, int32_t table_w);
+int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row_stride, int32_t dtype,
+                            const void* kp, const void* vp, const uint8_t* ks, const uint8_t* vs,
+                            int64_t n_pages, const int32_t* table, int32_t table_w,
+                            const int32_t* lens, const int32_t* qpos, int32_t rows, int32_t S,
+                            int32_t heads, int32_t kv_heads, int32_t dh, float scale, void* out,
+                            int64_t ldo, int64_t o_row_stride, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ *
  * Launch tracing for measurement.  While enabled, every kernel launch of the

@@ -12,7 +12,8 @@ LIB_PATH = os.environ.get("NV_LIB_PATH") or os.path.join(HERE, "libnv.so")
 
 NV_OK, NV_ERR_INVALID_ARG, NV_ERR_UNSUPPORTED = 0, -1, -2
 NV_ERR_OUT_OF_MEMORY, NV_ERR_HIP, NV_ERR_WORKSPACE = -3, -4, -5
-NV_F32, NV_BF16 = 0, 1
+NV_F32, NV_BF16, NV_F16 = 0, 1, 2
+NV_KV8_PAGE = 64
 NV_LOOKUP_STATIC_BYTES = 64 << 20
 NV_FAM_CONV, NV_FAM_LINEAR, NV_FAM_ATTN, NV_FAM_SCAN = 1, 2, 4, 8
 NV_UNET_GRAPHS = 1
@@ -94,6 +95,17 @@ _sigs = {
                             VP]),
     "nv_op_attention": (I32, [VP, VP, VP, VP, I32, I32, I32, I32, I32, I32, I32, I32, I64, I64,
                               F32, VP]),
+    "nv_op_quant8": (I32, [VP, I32, I64, I64, I32, I32, VP, I64, VP, VP]),
+    "nv_op_dequant8": (I32, [VP, I64, VP, I64, I32, I32, VP, I32, I64, VP]),
+    "nv_op_rmsnorm8": (I32, [VP, I64, VP, I64, I32, VP, F32, I64, I32, VP, I64, VP, I64, VP, VP]),
+    "nv_op_linear8_workspace": (SZ, [I64, I32, I32]),
+    "nv_op_linear8": (I32, [VP, I64, VP, VP, I64, VP, VP, VP, I64, VP, I64, I32, I64, I32, I32,
+                            VP, SZ, VP]),
+    "nv_op_kv8_append": (I32, [VP, I64, I64, VP, I64, I64, I32, I32, I32, I32, I32, VP, VP, VP,
+                               VP, I64, VP, I32, VP, VP, VP]),
+    "nv_op_attention_kv8_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
+    "nv_op_attention_kv8": (I32, [VP, I64, I64, I32, VP, VP, VP, VP, I64, VP, I32, VP, VP, I32,
+                                  I32, I32, I32, I32, F32, VP, I64, I64, VP, SZ, VP]),
 }
 for _name, (_res, _args) in _sigs.items():
     _f = getattr(lib, _name)

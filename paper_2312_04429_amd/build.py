@@ -13,7 +13,8 @@ SRC = os.environ.get("NV_BUILD_SRC") or os.path.join(HERE, "csrc")
 OUT_DIR = os.environ.get("NV_BUILD_DIR") or os.path.join(HERE, "_build")
 LIB = os.environ.get("NV_BUILD_OUT") or os.path.join(HERE, "libnv.so")
 SOURCES = ["lookup.hip", "gemm.hip", "attention.hip", "ops.hip", "unet.hip", "trace.hip",
-           "probe.hip", "pool.hip", "lcbfu.cpp", "predictor.hip", "ivf.hip"]
+           "probe.hip", "pool.hip", "lcbfu.cpp", "predictor.hip", "ivf.hip", "quant8.hip",
+           "linear8.hip", "kv8.hip"]
 ARCH = os.environ.get("NV_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -1,0 +1,597 @@
+// Keys and values kept in 8 bits: appending tokens to their pages, and attention over them.
+//
+// Page: 64 tokens of one sequence.  Keys [head][64][dh] and values [head][dh][64] as e4m3
+// codes, one scale byte per page and head for each.
+//
+// Attention multiplies float16 (or bfloat16) matrices: codes convert exactly (three mantissa
+// bits), queries are taken as they are, and scales stay out of the 16-bit operands: a page's key
+// scale multiplies its scores in float32, its value scale the accumulators' common unit.
+// S^T = K Q^T is computed, so an accumulator entry's column is a query and the softmax state is a
+// lane's own; key row r of 16-key tile t is token 16 (r / 4) + 4 t + r % 4 of the page, so that
+// lane group kc ends up with tokens 16 kc .. 16 kc + 15: the probabilities are then the second
+// product's operand as they stand, against 16 consecutive bytes of a value row.  Nothing passes
+// through LDS until waves merge.
+#include <algorithm>
+
+#include "common.h"
+#include "e4m3.h"
+#include "kv8.h"
+
+namespace nv {
+namespace {
+
+constexpr int PAGE = NV_KV8_PAGE;
+constexpr float LOG2E = 1.4426950408889634f;
+
+// ------------------------------------------------------------------------------------ append
+
+// Four codes at another scale (old value * 2^d, d < 0).
+__device__ __forceinline__ uint32_t recode4(uint32_t w, float f) {
+  const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+  const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return codes4(a[0], a[1], b[0], b[1], f);
+}
+
+// A workgroup per (row, touched page, head) and tensor: the new tokens' values stay in registers
+// between their largest magnitude and their codes.  Bound by latency for single tokens, by HBM
+// for prompts (the value codes are transposed in LDS and leave as 4-byte words).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) kv8_append_k(Kv8AppendArgs a) {
+  constexpr int MAXU = 64 * 160 / 8 / 256;  // eights of new values a thread can hold
+  __shared__ float part[4];
+  __shared__ __align__(16) uint8_t tr[160 * 68];  // [channel][64 tokens], rows 68 bytes apart
+  const int tid = threadIdx.x, head = blockIdx.y >> 1;
+  const bool is_v = blockIdx.y & 1;
+  const int64_t row = blockIdx.z;
+  const int64_t pos = a.pos[row];
+  const int cnt = a.count ? std::min(std::max(a.count[row], 0), a.T) : a.T;
+  if (pos < 0) return;
+  const int64_t p = pos / PAGE + blockIdx.x, first = p * PAGE;
+  const int64_t lo = std::max(pos, first), hi = std::min(pos + cnt, first + PAGE);
+  if (lo >= hi || p >= a.table_w) return;
+  const int64_t page = a.table[row * a.table_w + p];
+  if (page < 0 || page >= a.n_pages) return;
+  const int t0 = (int)(lo - first), t1 = (int)(hi - first);  // new tokens of the page
+  const int dh = a.dh, nch = dh / 8, units = (t1 - t0) * nch;
+  const T* src = (const T*)(is_v ? a.v + row * a.v_row * sizeof(T) : a.k + row * a.k_row * sizeof(T));
+  const int64_t ld = is_v ? a.ldv : a.ldk;
+  src += (lo - pos) * ld + (int64_t)head * dh;
+  const int64_t ph = page * a.heads + head;
+  uint8_t* codes = (is_v ? a.vp : a.kp) + ph * PAGE * dh;
+  uint8_t* scale = (is_v ? a.vs : a.ks) + ph;
+
+  float v[MAXU][8];
+  float top = 0.f;
+#pragma unroll
+  for (int u = 0; u < MAXU; ++u) {
+    const int i = u * 256 + tid;
+    if (u * 256 >= units) break;  // uniform
+    const int t = i / nch, c = (i - t * nch) * 8;
+    load8<VEC>(src + t * ld, c, i < units ? dh : 0, v[u]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[u][j]));
+  }
+  top = rows_max(row16_max(top));
+  if ((tid & 63) == 0) part[tid >> 6] = top;
+  const int old = t0 > 0 ? *scale : 0;
+  __syncthreads();  // the old scale has been read, too
+  const int e = std::max(old, scale_byte(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]))));
+  const float inv = ldexpf(1.f, 127 - e), move = ldexpf(1.f, old - e);
+  const bool grow = t0 > 0 && e > old;
+  if (tid == 0 && (t0 == 0 || grow)) *scale = (uint8_t)e;
+  if (!is_v) {
+    if (grow)
+      for (int i = tid; i < t0 * nch; i += 256) {
+        uint2* w = (uint2*)(codes + i * 8);
+        *w = make_uint2(recode4(w->x, move), recode4(w->y, move));
+      }
+#pragma unroll
+    for (int u = 0; u < MAXU; ++u) {
+      const int i = u * 256 + tid;
+      if (u * 256 >= units) break;
+      if (i < units) store_codes8<true>(codes + t0 * dh, i * 8, units * 8, v[u], inv);
+    }
+    return;
+  }
+#pragma unroll
+  for (int u = 0; u < MAXU; ++u) {
+    const int i = u * 256 + tid;
+    if (u * 256 >= units) break;
+    const int t = i / nch, c = (i - t * nch) * 8;
+    if (i < units) {
+      const uint32_t w0 = codes4(v[u][0], v[u][1], v[u][2], v[u][3], inv);
+      const uint32_t w1 = codes4(v[u][4], v[u][5], v[u][6], v[u][7], inv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        tr[(c + j) * 68 + t0 + t] = (uint8_t)((j < 4 ? w0 : w1) >> (8 * (j & 3)));
+    }
+  }
+  __syncthreads();
+  // words of four tokens: new codes within [t0, t1), old ones (moved if the scale grew) before,
+  // what was there behind
+  const int w0 = (grow ? 0 : t0) / 4, nw = (t1 + 3) / 4 - w0;
+  for (int i = tid; i < dh * nw; i += 256) {
+    const int c = i / nw, t = (w0 + i - c * nw) * 4;
+    uint32_t* to = (uint32_t*)(codes + c * PAGE + t);
+    uint32_t fresh = *(const uint32_t*)(tr + c * 68 + t);
+    if (t < t0 || t + 4 > t1) {
+      const uint32_t was = *to;
+      const uint32_t kept = grow ? recode4(was, move) : was;
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t m = 0xFFu << (8 * j);
+        w |= (t + j < t0 ? kept : t + j < t1 ? fresh : was) & m;
+      }
+      fresh = w;
+    }
+    *to = fresh;
+  }
+}
+
+// --------------------------------------------------------------------------------- attention
+
+// Four pairs of 16-bit values as one operand.
+template <typename Vec, typename P>
+__device__ __forceinline__ Vec pack8(P a, P b, P c, P d) {
+  return __builtin_bit_cast(Vec, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                                       __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
+}
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<_Float16> {
+  typedef half8 Vec;
+  static __device__ __forceinline__ floatx4 mul(Vec a, Vec b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  // eight codes times the power of two s
+  static __device__ __forceinline__ Vec codes(uint32_t lo, uint32_t hi, float s) {
+    return pack8<Vec>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, s, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, s, true),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, s, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, s, true));
+  }
+};
+template <>
+struct Mma<__bf16> {
+  typedef bf16x8 Vec;
+  static __device__ __forceinline__ floatx4 mul(Vec a, Vec b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ Vec codes(uint32_t lo, uint32_t hi, float s) {
+    return pack8<Vec>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
+                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false),
+                      __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true));
+  }
+};
+
+// Head dimension in 32-wide steps.  A whole 64 is two steps of which lane group kc takes dims
+// 16 kc .. 16 kc + 15 (one 16-byte load); the rest go 8 a group, dims past dh zero.
+template <int DH>
+struct Dims {
+  static constexpr int FULL = DH / 64, REST = DH % 64, STEPS = 2 * FULL + (REST + 31) / 32;
+  static constexpr int DV = (DH + 15) / 16;  // 16-channel tiles of the output
+  static __device__ __forceinline__ int dim(int step, int kc) {
+    return step < 2 * FULL ? (step / 2) * 64 + kc * 16 + (step & 1) * 8
+                           : FULL * 64 + (step - 2 * FULL) * 32 + kc * 8;
+  }
+};
+
+// Bytes of w (tokens t .. t + 15) at or past n tokens become zero.
+__device__ __forceinline__ u32x4 keep_tokens(u32x4 w, int n) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int k = n - j * 4;
+    if (k < 4) w[j] = k <= 0 ? 0 : w[j] & ((1u << (8 * k)) - 1);
+  }
+  return w;
+}
+
+// Nonzero where a byte of w is a NaN code (0x7F, 0xFF): that byte's bit 7.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+}
+
+// One wave's running softmax over 16 queries: reference maximum, this lane's share of the sum,
+// accumulators O^T in units of 2^(unit - 127).
+template <int DH>
+struct State {
+  float m, l;
+  int unit;
+  floatx4 acc[Dims<DH>::DV];
+};
+
+// The value exponents that convert exactly beside the unit: codes are 2^-9 .. 448, times
+// 2^-5 .. 2^7 still normal float16 numbers.
+constexpr int UNIT_LO = -5, UNIT_HI = 7;
+
+// A page's 64 tokens, from token j0 of the sequence, into the state.  lim: tokens this lane's
+// query sees; len: tokens of the sequence; some: whether some query sees only part of them.
+template <typename T, int DH>
+__device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::Vec* fq,
+                                          const uint8_t* kp, const uint8_t* vp, int ke, int ve,
+                                          float scale2, int j0, int lim, int len, bool some,
+                                          int li, int kc) {
+  using D = Dims<DH>;
+  using M = Mma<T>;
+  typedef typename M::Vec Vec;
+  floatx4 s[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint8_t* kr = kp + (16 * (li >> 2) + 4 * t + (li & 3)) * DH;
+    s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < D::FULL; ++b) {
+      const u32x4 w = *(const u32x4*)(kr + b * 64 + kc * 16);
+      s[t] = M::mul(M::codes(w[0], w[1], 1.f), fq[2 * b], s[t]);
+      s[t] = M::mul(M::codes(w[2], w[3], 1.f), fq[2 * b + 1], s[t]);
+    }
+#pragma unroll
+    for (int b = 2 * D::FULL; b < D::STEPS; ++b) {
+      const int d = D::dim(b, kc);
+      uint2 w = make_uint2(0, 0);
+      if (d < DH) w = *(const uint2*)(kr + d);
+      s[t] = M::mul(M::codes(w.x, w.y, 1.f), fq[b], s[t]);
+    }
+  }
+  u32x4 v[D::DV];
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) {
+    const int c = j * 16 + li;
+    v[j] = DH % 16 == 0 || c < DH ? *(const u32x4*)(vp + c * PAGE + kc * 16) : u32x4{0, 0, 0, 0};
+  }
+  const float f = scale2 * scale_value(ke);
+  float top = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[t][r] *= f;
+      if (some && j0 + 16 * kc + 4 * t + r >= lim) s[t][r] = -INFINITY;
+      top = fmaxf(top, s[t][r]);
+    }
+  const float mnew = fmaxf(st.m, rows_max(top)), base = mnew == -INFINITY ? 0.f : mnew;
+  const float alpha = __builtin_amdgcn_exp2f(st.m - base);
+  if (__ballot(mnew != st.m)) {
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) st.acc[j] *= alpha;
+    st.l *= alpha;
+    st.m = mnew;
+  }
+  Vec fp[2];
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float p = __builtin_amdgcn_exp2f(s[t][r] - base);
+      sum += p;
+      fp[t >> 1][(t & 1) * 4 + r] = (T)p;
+    }
+  st.l += sum;
+  if (ve == 255) {  // a NaN scale: every code of the page is NaN, the unit stays
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) v[j] = u32x4{0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F};
+    ve = st.unit;
+  }
+  if (some) {
+    // Tokens behind the sequence may hold anything: zeros.  A NaN among those before that some
+    // query does not see must not reach it (0 * NaN): NaN codes become zeros, and a product of
+    // indicators (is NaN) x (is seen) finds the outputs that they do reach.
+    uint32_t any = 0;
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) {
+      v[j] = keep_tokens(v[j], len - j0 - kc * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) any |= nan_bytes(v[j][i]);
+    }
+    if (__ballot(any != 0)) {
+      Vec seen[2];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          seen[t >> 1][(t & 1) * 4 + r] = (T)(j0 + 16 * kc + 4 * t + r < lim ? 1.f : 0.f);
+#pragma unroll
+      for (int j = 0; j < D::DV; ++j) {
+        u32x4 ind;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t n = nan_bytes(v[j][i]) >> 7;  // 1 in each NaN byte
+          ind[i] = n * 0x38;                           // code of 1.0
+          v[j][i] &= ~(n * 0xFF);
+        }
+        floatx4 hit = {0.f, 0.f, 0.f, 0.f};
+        hit = M::mul(M::codes(ind[0], ind[1], 1.f), seen[0], hit);
+        hit = M::mul(M::codes(ind[2], ind[3], 1.f), seen[1], hit);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (hit[r] > 0.f) st.acc[j][r] = __int_as_float(0x7FC00000);
+      }
+    }
+  }
+  int d = ve - st.unit;
+  if (d < UNIT_LO) {  // far below the unit: its own accumulators, added at their size
+    const float g = ldexpf(1.f, d);
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) {
+      floatx4 o = {0.f, 0.f, 0.f, 0.f};
+      o = M::mul(M::codes(v[j][0], v[j][1], 1.f), fp[0], o);
+      o = M::mul(M::codes(v[j][2], v[j][3], 1.f), fp[1], o);
+      st.acc[j] += o * g;
+    }
+    return;
+  }
+  if (d > UNIT_HI) {  // far above: it becomes the unit
+    const float g = ldexpf(1.f, -d);
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) st.acc[j] *= g;
+    st.unit = ve;
+    d = 0;
+  }
+  const float g = __int_as_float((127 + d) << 23);
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) {
+    st.acc[j] = M::mul(M::codes(v[j][0], v[j][1], g), fp[0], st.acc[j]);
+    st.acc[j] = M::mul(M::codes(v[j][2], v[j][3], g), fp[1], st.acc[j]);
+  }
+}
+
+// A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and a
+// share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
+// than one share the sums go to the workspace and attn_kv8_join_k adds them in order.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
+  using D = Dims<DH>;
+  typedef typename Mma<T>::Vec Vec;
+  constexpr int NW = 4, CH = D::DV * 16;
+  __shared__ float sm[NW][16], sl[NW][16];
+  __shared__ __align__(16) float so[NW][16][CH + 4];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int id = blockIdx.x;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int ct = id % a.col_tiles;
+  id /= a.col_tiles;
+  const int head = id % a.kv_heads, row = id / a.kv_heads;
+  const int group = a.heads / a.kv_heads, cols = a.S * group, c0 = ct * 16;
+  const int col = std::min(c0 + li, cols - 1), qs = col / group, qh = head * group + col % group;
+  const int len = (int)std::min<int64_t>(std::max(a.lens[row], 0), (int64_t)a.table_w * PAGE);
+  const int64_t q0 = a.qpos ? (int64_t)a.qpos[row] + 1 : len;  // tokens that query 0 sees
+  auto sees = [&](int s) {
+    return (int)std::max<int64_t>(0, std::min<int64_t>(len, a.qpos ? q0 + s : len));
+  };
+  const int lim = sees(qs), least = sees(c0 / group);
+  const int most = sees((std::min(c0 + 16, cols) - 1) / group);
+  const int pages = (most + PAGE - 1) / PAGE;
+  const int p0 = (int)((int64_t)pages * split / a.splits);
+  const int p1 = (int)((int64_t)pages * (split + 1) / a.splits);
+
+  Vec fq[D::STEPS];
+  const T* qrow = (const T*)a.q + (int64_t)row * a.q_row + (int64_t)qs * a.ldq + (int64_t)qh * DH;
+#pragma unroll
+  for (int b = 0; b < D::STEPS; ++b) {
+    const int d = D::dim(b, kc);
+    fq[b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
+  }
+  State<DH> st;
+  st.m = -INFINITY, st.l = 0.f, st.unit = 1;
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) st.acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const float scale2 = a.scale * LOG2E;
+  for (int p = p0 + wave; p < p1; p += NW) {
+    const int64_t page = a.table[(int64_t)row * a.table_w + p];
+    if (page < 0 || page >= a.n_pages) continue;
+    const int64_t ph = page * a.kv_heads + head;
+    page_step<T, DH>(st, fq, a.kp + ph * PAGE * DH, a.vp + ph * PAGE * DH, a.ks[ph], a.vs[ph],
+                     scale2, p * PAGE, lim, len, p * PAGE + PAGE > least, li, kc);
+  }
+  // the waves' states, in wave order
+  const float l = rows_sum(st.l), us = scale_value(st.unit);
+  if (kc == 0) sm[wave][li] = st.m, sl[wave][li] = l;
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) *(floatx4*)&so[wave][li][j * 16 + kc * 4] = st.acc[j] * us;
+  __syncthreads();
+  for (int i = tid; i < 16 * (CH / 4); i += 256) {
+    const int c = i / (CH / 4), d = i % (CH / 4) * 4;
+    if (c0 + c >= cols || d >= DH) continue;
+    float m = sm[0][c];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][c]);
+    const float base = m == -INFINITY ? 0.f : m;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    float ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][c] - base);
+      ls += f * sl[w][c];
+      o += f * *(const floatx4*)&so[w][c][d];
+    }
+    if (a.splits == 1) {
+      const int qi = (c0 + c) / group, h = head * group + (c0 + c) % group;
+      struct alignas(8) Quad { T v[4]; } out;
+      const float inv = ls == 0.f ? 0.f : 1.f / ls;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+      *(Quad*)((T*)a.out + (int64_t)row * a.o_row + (int64_t)qi * a.ldo + (int64_t)h * DH + d) = out;
+    } else {
+      const int64_t slot = (((int64_t)row * a.kv_heads + head) * cols + c0 + c) * a.splits + split;
+      *(floatx4*)(a.part_o + slot * DH + d) = o;
+      if (d == 0) a.part_ml[slot * 2] = m, a.part_ml[slot * 2 + 1] = ls;
+    }
+  }
+}
+
+// Shares of a query's pages, in order: one thread per four channels.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
+  const int group = a.heads / a.kv_heads, nq = a.dh / 4;
+  const int64_t cols = (int64_t)a.S * group, total = a.rows * a.kv_heads * cols * nq;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t u = i / nq, rh = u / cols, c = u - rh * cols;
+    const int d = (int)(i - u * nq) * 4;
+    const float* ml = a.part_ml + u * a.splits * 2;
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s * 2]);
+    const float base = m == -INFINITY ? 0.f : m;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    float ls = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = __builtin_amdgcn_exp2f(ml[s * 2] - base);
+      ls += f * ml[s * 2 + 1];
+      o += f * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
+    }
+    const int64_t row = rh / a.kv_heads, h = rh % a.kv_heads * group + c % group;
+    struct alignas(8) Quad { T v[4]; } out;
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+    *(Quad*)((T*)a.out + row * a.o_row + c / group * a.ldo + h * a.dh + d) = out;
+  }
+}
+
+template <typename T, int DH>
+hipError_t attn_go(const Kv8AttnArgs& a, hipStream_t s) {
+  const int64_t wgs = (int64_t)a.rows * a.kv_heads * a.col_tiles * a.splits;
+  hipLaunchKernelGGL((attn_kv8_k<T, DH>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  if (a.splits > 1) {
+    const int64_t n = (int64_t)a.rows * a.heads * a.S * (DH / 4);
+    hipLaunchKernelGGL(attn_kv8_join_k<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 20)),
+                       dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attn_launch_t(const Kv8AttnArgs& a, hipStream_t s) {
+  switch (a.dh) {
+    case 16: return attn_go<T, 16>(a, s);
+    case 32: return attn_go<T, 32>(a, s);
+    case 40: return attn_go<T, 40>(a, s);
+    case 64: return attn_go<T, 64>(a, s);
+    case 80: return attn_go<T, 80>(a, s);
+    case 128: return attn_go<T, 128>(a, s);
+    case 160: return attn_go<T, 160>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+bool head_dim_ok(int dh) {
+  return dh == 16 || dh == 32 || dh == 40 || dh == 64 || dh == 80 || dh == 128 || dh == 160;
+}
+
+size_t part_bytes(const Kv8Plan& p, int64_t queries, int dh, size_t* ml_at) {
+  const size_t o = align_up((size_t)queries * p.splits * dh * 4, 256);
+  if (ml_at) *ml_at = o;
+  return p.splits > 1 ? o + align_up((size_t)queries * p.splits * 8, 256) : 0;
+}
+
+}  // namespace
+}  // namespace nv
+
+using namespace nv;
+
+extern "C" int32_t nv_op_kv8_append(const void* k, int64_t ldk, int64_t k_row_stride, const void* v,
+                                    int64_t ldv, int64_t v_row_stride, int32_t dtype, int32_t rows,
+                                    int32_t T, int32_t heads, int32_t dh, void* kp, void* vp,
+                                    uint8_t* ks, uint8_t* vs, int64_t n_pages,
+                                    const int32_t* table, int32_t table_w, const int32_t* pos,
+                                    const int32_t* count, void* stream) {
+  clear_error();
+  NV_CHECK_ARG(rows >= 0 && rows <= 65535 && T >= 0 && heads >= 1 && heads <= 32767,
+               "need 0 <= rows <= 65535, T >= 0 and 1 <= heads <= 32767");
+  NV_CHECK_ARG(dtype == NV_F16 || dtype == NV_BF16, "dtype must be NV_F16 or NV_BF16");
+  NV_CHECK_ARG(n_pages >= 0 && table_w >= 0, "negative sizes");
+  NV_CHECK_ARG(ldk >= 0 && ldv >= 0 && k_row_stride >= 0 && v_row_stride >= 0, "negative strides");
+  if (!head_dim_ok(dh)) {
+    set_error("dh must be 16, 32, 40, 64, 80, 128 or 160");
+    return NV_ERR_UNSUPPORTED;
+  }
+  if (rows == 0 || T == 0 || n_pages == 0 || table_w == 0) return NV_OK;
+  NV_CHECK_ARG(k && v && kp && vp && ks && vs && table && pos, "null pointer argument");
+  NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
+  const Kv8AppendArgs a{(const uint8_t*)k, (const uint8_t*)v, (uint8_t*)kp, (uint8_t*)vp, ks, vs,
+                        ldk, k_row_stride, ldv, v_row_stride, n_pages, table, pos, count,
+                        T, heads, dh, table_w};
+  const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
+  const int64_t touched = std::min<int64_t>(((int64_t)T + PAGE - 2) / PAGE + 1, table_w);
+  const dim3 grid((unsigned)touched, heads * 2, rows);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+  };
+  if (dtype == NV_F16) vec ? go(kv8_append_k<_Float16, true>) : go(kv8_append_k<_Float16, false>);
+  else vec ? go(kv8_append_k<__bf16, true>) : go(kv8_append_k<__bf16, false>);
+  NV_LAUNCH_CHECK("kv8_append_k");
+  return NV_OK;
+}
+
+extern "C" size_t nv_op_attention_kv8_workspace(int32_t rows, int32_t S, int32_t heads,
+                                                int32_t kv_heads, int32_t dh, int32_t table_w) {
+  if (rows < 1 || S < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || !head_dim_ok(dh) ||
+      table_w < 0)
+    return 0;
+  return part_bytes(kv8_plan(rows, S, heads, kv_heads, table_w), (int64_t)rows * S * heads, dh,
+                    nullptr);
+}
+
+extern "C" int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row_stride,
+                                       int32_t dtype, const void* kp, const void* vp,
+                                       const uint8_t* ks, const uint8_t* vs, int64_t n_pages,
+                                       const int32_t* table, int32_t table_w, const int32_t* lens,
+                                       const int32_t* qpos, int32_t rows, int32_t S, int32_t heads,
+                                       int32_t kv_heads, int32_t dh, float scale, void* out,
+                                       int64_t ldo, int64_t o_row_stride, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  clear_error();
+  NV_CHECK_ARG(rows >= 0 && S >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0,
+               "need rows, S >= 0 and heads a positive multiple of kv_heads");
+  NV_CHECK_ARG(dtype == NV_F16 || dtype == NV_BF16, "dtype must be NV_F16 or NV_BF16");
+  NV_CHECK_ARG(n_pages >= 0 && table_w >= 0 && table_w <= 0x7FFFFFFF / PAGE,
+               "need n_pages >= 0 and 0 <= table_w < 2^25");
+  NV_CHECK_ARG(scale - scale == 0.f, "scale must be finite");
+  if (!head_dim_ok(dh)) {
+    set_error("dh must be 16, 32, 40, 64, 80, 128 or 160");
+    return NV_ERR_UNSUPPORTED;
+  }
+  NV_CHECK_ARG(ldq >= 0 && q_row_stride >= 0 && ldo >= (int64_t)heads * dh && o_row_stride >= 0,
+               "negative strides, or rows of out shorter than heads * dh");
+  if (rows == 0 || S == 0) return NV_OK;
+  NV_CHECK_ARG(q && lens && out && (table_w == 0 || table) &&
+                   (n_pages == 0 || (kp && vp && ks && vs)), "null pointer argument");
+  if ((ldq | q_row_stride | ldo | o_row_stride) % 8 || !aligned16(q) || !aligned16(out)) {
+    set_error("q and out need 16-byte aligned buffers and strides in multiples of 8");
+    return NV_ERR_UNSUPPORTED;
+  }
+  NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
+  const Kv8Plan p = kv8_plan(rows, S, heads, kv_heads, table_w);
+  if ((int64_t)S * (heads / kv_heads) > 0x7FFFFFF0 ||
+      (double)rows * kv_heads * p.col_tiles * p.splits > 8388607.0) {
+    set_error("more queries than a grid holds");
+    return NV_ERR_UNSUPPORTED;
+  }
+  size_t ml_at = 0;
+  const size_t need = part_bytes(p, (int64_t)rows * S * heads, dh, &ml_at);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) {
+    set_error("workspace missing, misaligned or smaller than nv_op_attention_kv8_workspace()");
+    return NV_ERR_WORKSPACE;
+  }
+  Kv8AttnArgs a{};
+  a.q = q, a.ldq = ldq, a.q_row = q_row_stride;
+  a.kp = (const uint8_t*)kp, a.vp = (const uint8_t*)vp, a.ks = ks, a.vs = vs;
+  a.n_pages = n_pages, a.table = table, a.table_w = table_w, a.lens = lens, a.qpos = qpos;
+  a.rows = rows, a.S = S, a.heads = heads, a.kv_heads = kv_heads, a.dh = dh, a.scale = scale;
+  a.out = out, a.ldo = ldo, a.o_row = o_row_stride;
+  a.col_tiles = p.col_tiles, a.splits = p.splits;
+  if (need) {
+    a.part_o = (float*)workspace;
+    a.part_ml = (float*)((uint8_t*)workspace + ml_at);
+  }
+  const hipStream_t s = (hipStream_t)stream;
+  NV_HIP_TRY(dtype == NV_F16 ? attn_launch_t<_Float16>(a, s) : attn_launch_t<__bf16>(a, s));
+  return NV_OK;
+}

@@ -1,0 +1,167 @@
+"""The 8-bit operators without a GPU: the oracle's 8-bit form against torch's own e4m3 type, and
+every refusal of the C entry points and their Python wrappers (nothing is launched)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops8 as O
+
+
+def test_oracle_codes_are_torchs_e4m3():
+    codes = torch.arange(256, dtype=torch.uint8)
+    v = codes.view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(v, O.VALUES, equal_nan=True)
+    rng = np.random.default_rng(0)
+    x = np.concatenate([rng.uniform(-448, 448, 4000), rng.standard_normal(4000) * 0.02,
+                        O.VALUES[:127], (O.VALUES[:126] + O.VALUES[1:127]) / 2, [-0.0, np.nan]])
+    x = x.astype(np.float32)
+    t = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    got = O.encode(x)
+    assert np.array_equal(got & 127, t & 127)
+    assert np.array_equal(got[~np.isnan(x)], t[~np.isnan(x)])
+
+
+def test_oracle_scale_is_the_smallest_that_fits():
+    rng = np.random.default_rng(1)
+    a = np.concatenate([np.exp2(rng.uniform(-110, 120, 2000)), 448 * np.exp2(np.arange(-90., 90.)),
+                        448 * np.exp2(np.arange(-90., 90.)) * (1 + 2 ** -23)])
+    e = O.scale_byte(a)
+    assert (a <= 448 * O.scale_value(e)).all()
+    assert (a > 448 * O.scale_value(e - 1))[e > 1].all()
+    assert O.scale_byte(0.0) == 1 and np.isnan(O.scale_value(255))
+
+
+def test_oracle_append_keeps_what_it_should():
+    rng = np.random.default_rng(2)
+    codes, scales = rng.integers(0, 120, (4, 1, 64, 16)).astype(np.uint8), np.full((4, 1), 120, np.uint8)
+    x = rng.standard_normal((1, 3, 1, 16))
+    c, s = O.append(x, codes, scales, np.array([[2, -1]]), [62], [3], False)
+    assert np.array_equal(c[[0, 1, 3]], codes[[0, 1, 3]]) and np.array_equal(s[[0, 1, 3]], scales[[0, 1, 3]])
+    assert np.array_equal(c[2, 0, 62:], O.encode(x[0, :2, 0] * 2.0 ** (127 - int(s[2, 0]))))
+
+
+# ------------------------------------------------------------------------------- refusals
+
+D = C.c_void_p(0x10000)      # never read: every call here ends before a launch
+ODD = C.c_void_p(0x10004)
+
+
+def _lib():
+    from paper_2312_04429_amd import _native as N
+    return N
+
+
+def test_quant8_refusals():
+    N = _lib()
+
+    def call(x=D, dt=N.NV_F16, ldx=256, M=4, K=256, br=1, q=D, ldq=256, s=D):
+        return N.lib.nv_op_quant8(x, dt, ldx, M, K, br, q, ldq, s, None)
+    for bad in (dict(x=None), dict(q=None), dict(s=None), dict(dt=7), dict(M=-1), dict(K=0),
+                dict(br=2), dict(ldx=255), dict(ldq=255)):
+        assert call(**bad) == N.NV_ERR_INVALID_ARG, bad
+    assert call(M=0, x=None) == N.NV_OK
+
+    def back(q=D, ldq=256, s=D, M=4, K=256, br=1, out=D, dt=N.NV_F16, ldo=256):
+        return N.lib.nv_op_dequant8(q, ldq, s, M, K, br, out, dt, ldo, None)
+    for bad in (dict(q=None), dict(s=None), dict(out=None), dict(dt=-1), dict(M=-1), dict(K=0),
+                dict(br=0), dict(ldq=1), dict(ldo=255)):
+        assert back(**bad) == N.NV_ERR_INVALID_ARG, bad
+    assert back(M=0) == N.NV_OK
+
+
+def test_rmsnorm8_refusals():
+    N = _lib()
+
+    def call(x=D, ldx=64, r=None, ldr=0, dt=N.NV_F16, w=D, eps=1e-6, M=2, Dm=64, h=None, ldh=0, q=D,
+             ldq=64, s=D):
+        return N.lib.nv_op_rmsnorm8(x, ldx, r, ldr, dt, w, eps, M, Dm, h, ldh, q, ldq, s, None)
+    for bad in (dict(x=None), dict(w=None), dict(q=None), dict(s=None), dict(dt=N.NV_F32),
+                dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(M=-1),
+                dict(Dm=0), dict(ldx=63), dict(ldq=63), dict(r=D, ldr=63), dict(h=D, ldh=63)):
+        assert call(**bad) == N.NV_ERR_INVALID_ARG, bad
+    assert call(Dm=32769, ldx=40000, ldq=40000) == N.NV_ERR_UNSUPPORTED
+    assert call(M=0) == N.NV_OK
+
+
+def test_linear8_refusals():
+    N = _lib()
+
+    def call(x=D, ldx=256, xs=D, w=D, ldw=256, ws=D, b=None, r=None, ldr=0, out=D, ldo=64,
+             dt=N.NV_F16, M=4, Nn=64, K=256, wsp=D, wsb=1 << 40):
+        return N.lib.nv_op_linear8(x, ldx, xs, w, ldw, ws, b, r, ldr, out, ldo, dt, M, Nn, K, wsp,
+                                   wsb, None)
+    for bad in (dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(out=None),
+                dict(dt=N.NV_F32), dict(M=-1), dict(M=1 << 31), dict(Nn=0), dict(K=0),
+                dict(ldx=240), dict(ldw=240), dict(ldo=63), dict(r=D, ldr=63)):
+        assert call(**bad) == N.NV_ERR_INVALID_ARG, bad
+    for bad in (dict(ldx=264), dict(ldw=264), dict(x=ODD), dict(w=ODD), dict(ldx=(1 << 22) + 16)):
+        assert call(**bad) == N.NV_ERR_UNSUPPORTED, bad
+    assert call(M=0) == N.NV_OK
+    need = N.lib.nv_op_linear8_workspace(64, 256, 8192)
+    assert need > 0
+    big = dict(M=64, Nn=256, K=8192, ldx=8192, ldw=8192, ldo=256)
+    assert call(**big, wsb=need - 1) == N.NV_ERR_WORKSPACE
+    assert call(**big, wsp=None) == N.NV_ERR_WORKSPACE
+    assert call(**big, wsp=ODD) == N.NV_ERR_WORKSPACE
+    assert N.lib.nv_op_linear8_workspace(0, 256, 8192) == 0
+
+
+def test_append_refusals():
+    N = _lib()
+
+    def call(k=D, v=D, ld=64, rs=64, dt=N.NV_F16, rows=1, T=1, H=1, dh=64, kp=D, vp=D, ks=D, vs=D,
+             n=4, table=D, W=4, pos=D, count=None):
+        return N.lib.nv_op_kv8_append(k, ld, rs, v, ld, rs, dt, rows, T, H, dh, kp, vp, ks, vs, n,
+                                      table, W, pos, count, None)
+    for bad in (dict(k=None), dict(v=None), dict(kp=None), dict(vp=None), dict(ks=None),
+                dict(vs=None), dict(table=None), dict(pos=None), dict(dt=N.NV_F32), dict(rows=-1),
+                dict(rows=65536), dict(T=-1), dict(H=0), dict(H=40000), dict(n=-1), dict(W=-1),
+                dict(ld=-8), dict(rs=-8), dict(kp=ODD), dict(vp=ODD)):
+        assert call(**bad) == N.NV_ERR_INVALID_ARG, bad
+    assert call(dh=48) == N.NV_ERR_UNSUPPORTED
+    for empty in (dict(rows=0), dict(T=0), dict(n=0), dict(W=0)):
+        assert call(**empty) == N.NV_OK, empty
+
+
+def test_attention_kv8_refusals():
+    N = _lib()
+
+    def call(q=D, ldq=256, qr=256, dt=N.NV_F16, kp=D, vp=D, ks=D, vs=D, n=4, table=D, W=4, lens=D,
+             qpos=None, rows=1, S=1, H=4, Hk=2, dh=64, scale=0.1, out=D, ldo=256, orow=256, wsp=D,
+             wsb=1 << 40):
+        return N.lib.nv_op_attention_kv8(q, ldq, qr, dt, kp, vp, ks, vs, n, table, W, lens, qpos,
+                                         rows, S, H, Hk, dh, scale, out, ldo, orow, wsp, wsb, None)
+    for bad in (dict(q=None), dict(lens=None), dict(out=None), dict(table=None), dict(kp=None),
+                dict(vp=None), dict(ks=None), dict(vs=None), dict(dt=N.NV_F32), dict(rows=-1),
+                dict(S=-1), dict(H=0), dict(Hk=0), dict(Hk=3), dict(n=-1), dict(W=-1),
+                dict(W=1 << 25), dict(scale=float("nan")), dict(scale=float("inf")), dict(ldq=-8),
+                dict(qr=-8), dict(ldo=248), dict(orow=-8), dict(kp=ODD), dict(vp=ODD)):
+        assert call(**bad) == N.NV_ERR_INVALID_ARG, bad
+    for bad in (dict(dh=48), dict(ldq=260), dict(qr=260), dict(ldo=260), dict(orow=4), dict(q=ODD),
+                dict(out=ODD), dict(rows=1 << 30, S=1 << 20)):
+        assert call(**bad) == N.NV_ERR_UNSUPPORTED, bad
+    assert call(rows=0) == N.NV_OK and call(S=0) == N.NV_OK
+    need = N.lib.nv_op_attention_kv8_workspace(1, 1, 4, 2, 64, 1000)
+    assert need > 0
+    assert call(W=1000, wsb=need - 1) == N.NV_ERR_WORKSPACE
+    assert call(W=1000, wsp=None) == N.NV_ERR_WORKSPACE
+    assert call(W=1000, wsp=ODD) == N.NV_ERR_WORKSPACE
+    assert N.lib.nv_op_attention_kv8_workspace(1, 1, 4, 3, 64, 1000) == 0
+
+
+def test_wrappers_take_device_tensors_only():
+    import paper_2312_04429_amd as P
+    x, s = torch.zeros(2, 128, dtype=torch.float16), torch.zeros(2, 1, dtype=torch.uint8)
+    q = torch.zeros(2, 128, dtype=torch.uint8)
+    pages = P.nv_kv8_pages(2, 1, 64, "cpu")
+    assert [tuple(t.shape) for t in pages] == [(2, 1, 64, 64), (2, 1, 64, 64), (2, 1), (2, 1)]
+    i = torch.zeros(1, dtype=torch.int32)
+    for call in (lambda: P.nv_op_quant8(x), lambda: P.nv_op_dequant8(q, s),
+                 lambda: P.nv_op_rmsnorm8(x, torch.ones(128)),
+                 lambda: P.nv_op_linear8(q, s, q, s),
+                 lambda: P.nv_op_kv8_append(x[None], x[None], pages, i[None], i),
+                 lambda: P.nv_op_attention_kv8(x[None], pages, i[None], i, 1.0)):
+        with pytest.raises(ValueError, match="device"):
+            call()
