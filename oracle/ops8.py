@@ -52,15 +52,12 @@ def quantise(x, rows=1):
     """(codes [M][K], scale bytes [ceil(M / rows)][ceil(K / 128)]) of x [M][K]."""
     x = np.asarray(x, np.float64)
     M, K = x.shape
-    q = np.empty((M, K), np.uint8)
-    s = np.empty((-(-M // rows), -(-K // 128)), np.uint8)
-    for i in range(s.shape[0]):
-        for j in range(s.shape[1]):
-            b = x[i * rows:(i + 1) * rows, j * 128:(j + 1) * 128]
-            s[i, j] = scale_byte(np.abs(_finite(b)).max())
-            q[i * rows:(i + 1) * rows, j * 128:(j + 1) * 128] = encode(
-                np.where(np.isfinite(b), b, np.nan) / scale_value(s[i, j]))
-    return q, s
+    b = np.zeros((-(-M // rows) * rows, -(-K // 128) * 128))
+    b[:M, :K] = x
+    b = b.reshape(-1, rows, b.shape[1] // 128, 128)
+    s = scale_byte(np.abs(_finite(b)).max((1, 3)))
+    q = encode(np.where(np.isfinite(b), b, np.nan) / scale_value(s)[:, None, :, None])
+    return q.reshape(-1, b.shape[2] * 128)[:M, :K].copy(), s
 
 
 def values(q, s, rows=1):

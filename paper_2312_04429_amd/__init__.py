@@ -26,7 +26,7 @@ from .api import (NvIVF, NvLCBFU, NvUNet, nv_cache_insert, nv_cache_move_rows, n
                   nv_cache_lookup_static, nv_cache_lookup_workspace, nv_gather_states,
                   nv_kv8_pages, nv_op_attention, nv_op_attention_kv8,
                   nv_op_attention_kv8_workspace, nv_op_conv3x3, nv_op_dequant8, nv_op_kv8_append,
-                  nv_op_linear, nv_op_linear8, nv_op_linear8_workspace, nv_op_quant8,
+                  nv_op_linear, nv_op_linear8, nv_op_quant8,
                   nv_op_rmsnorm8, nv_probe_peaks, nv_trace_disable,
                   nv_trace_enable, nv_trace_read, nv_trace_records, nv_unet_param_count,
                   nv_unet_param_info, workspace)
@@ -39,6 +39,6 @@ __all__ = ["FAM_ATTN", "FAM_CONV", "FAM_LINEAR", "FAM_SCAN", "NvIVF", "NvLCBFU",
            "nv_table_update", "nv_cache_insert", "nv_cache_lookup", "nv_cache_lookup_gated", "nv_cache_lookup_gated_workspace", "nv_cache_lookup_static", "nv_cache_lookup_workspace", "nv_gather_states",
            "nv_kv8_pages", "nv_op_attention", "nv_op_attention_kv8",
            "nv_op_attention_kv8_workspace", "nv_op_conv3x3", "nv_op_dequant8", "nv_op_kv8_append",
-           "nv_op_linear", "nv_op_linear8", "nv_op_linear8_workspace", "nv_op_quant8",
+           "nv_op_linear", "nv_op_linear8", "nv_op_quant8",
            "nv_op_rmsnorm8", "nv_probe_peaks", "nv_trace_disable", "nv_trace_enable",
            "nv_trace_read", "nv_trace_records", "nv_unet_param_count", "nv_unet_param_info", "workspace"]

@@ -98,9 +98,8 @@ _sigs = {
     "nv_op_quant8": (I32, [VP, I32, I64, I64, I32, I32, VP, I64, VP, VP]),
     "nv_op_dequant8": (I32, [VP, I64, VP, I64, I32, I32, VP, I32, I64, VP]),
     "nv_op_rmsnorm8": (I32, [VP, I64, VP, I64, I32, VP, F32, I64, I32, VP, I64, VP, I64, VP, VP]),
-    "nv_op_linear8_workspace": (SZ, [I64, I32, I32]),
     "nv_op_linear8": (I32, [VP, I64, VP, VP, I64, VP, VP, VP, I64, VP, I64, I32, I64, I32, I32,
-                            VP, SZ, VP]),
+                            VP]),
     "nv_op_kv8_append": (I32, [VP, I64, I64, VP, I64, I64, I32, I32, I32, I32, I32, VP, VP, VP,
                                VP, I64, VP, I32, VP, VP, VP]),
     "nv_op_attention_kv8_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),

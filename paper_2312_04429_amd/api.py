@@ -661,16 +661,10 @@ def _ws_of(need, device, ws):
     return own, addr, need
 
 
-def nv_op_linear8_workspace(M, N_, K):
-    return int(N.lib.nv_op_linear8_workspace(M, N_, K))
-
-
-def nv_op_linear8(x, xs, w, ws, bias=None, residual=None, dtype=torch.float16, out=None,
-                  workspace=None):
+def nv_op_linear8(x, xs, w, ws, bias=None, residual=None, dtype=torch.float16, out=None):
     """out[M][N] = x[M][K] w[N][K]^T (+ bias) (+ residual) of 8-bit matrices: x with scales xs per
     128 columns of a row, w with scales ws per 128 x 128 (nv_op_quant8); bias float32, residual
-    and out of `dtype`.  workspace: (owner, address, bytes) of nv_op_linear8_workspace(M, N, K)
-    bytes, or None: one for this call."""
+    and out of `dtype`."""
     _want(x, "x", _CODES)
     _want(w, "w", _CODES, None, x)
     ldx, ldw = _ld(x, "x"), _ld(w, "w")
@@ -692,10 +686,8 @@ def nv_op_linear8(x, xs, w, ws, bias=None, residual=None, dtype=torch.float16, o
     # a row of one may start at any stride, one that the kernel takes included
     ldx, ldw = (-(-K // 16) * 16 if n < 2 else ld for ld, n in ((ldx, M), (ldw, Nn)))
     with _on(x):
-        _own, addr, need = _ws_of(nv_op_linear8_workspace(M, Nn, K), x.device, workspace)
         st = N.lib.nv_op_linear8(_p(x), ldx, _p(xs), _p(w), ldw, _p(ws), _p(bias), _p(residual),
-                                 ldr, _p(out), _ld(out, "out"), _DT[dtype], M, Nn, K,
-                                 C.c_void_p(addr), need, _stream())
+                                 ldr, _p(out), _ld(out, "out"), _DT[dtype], M, Nn, K, _stream())
     N.check(st, "nv_op_linear8")
     return out
 

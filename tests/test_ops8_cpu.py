@@ -1,12 +1,15 @@
 """The 8-bit operators without a GPU: the oracle's 8-bit form against torch's own e4m3 type, and
 every refusal of the C entry points and their Python wrappers (nothing is launched)."""
 import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 from oracle import ops8 as O
+from ops8_sizes import FORM_SIZES
 
 
 def test_oracle_codes_are_torchs_e4m3():
@@ -89,9 +92,8 @@ def test_linear8_refusals():
     N = _lib()
 
     def call(x=D, ldx=256, xs=D, w=D, ldw=256, ws=D, b=None, r=None, ldr=0, out=D, ldo=64,
-             dt=N.NV_F16, M=4, Nn=64, K=256, wsp=D, wsb=1 << 40):
-        return N.lib.nv_op_linear8(x, ldx, xs, w, ldw, ws, b, r, ldr, out, ldo, dt, M, Nn, K, wsp,
-                                   wsb, None)
+             dt=N.NV_F16, M=4, Nn=64, K=256):
+        return N.lib.nv_op_linear8(x, ldx, xs, w, ldw, ws, b, r, ldr, out, ldo, dt, M, Nn, K, None)
     for bad in (dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(out=None),
                 dict(dt=N.NV_F32), dict(M=-1), dict(M=1 << 31), dict(Nn=0), dict(K=0),
                 dict(ldx=240), dict(ldw=240), dict(ldo=63), dict(r=D, ldr=63)):
@@ -99,13 +101,7 @@ def test_linear8_refusals():
     for bad in (dict(ldx=264), dict(ldw=264), dict(x=ODD), dict(w=ODD), dict(ldx=(1 << 22) + 16)):
         assert call(**bad) == N.NV_ERR_UNSUPPORTED, bad
     assert call(M=0) == N.NV_OK
-    need = N.lib.nv_op_linear8_workspace(64, 256, 8192)
-    assert need > 0
-    big = dict(M=64, Nn=256, K=8192, ldx=8192, ldw=8192, ldo=256)
-    assert call(**big, wsb=need - 1) == N.NV_ERR_WORKSPACE
-    assert call(**big, wsp=None) == N.NV_ERR_WORKSPACE
-    assert call(**big, wsp=ODD) == N.NV_ERR_WORKSPACE
-    assert N.lib.nv_op_linear8_workspace(0, 256, 8192) == 0
+    assert call(M=(1 << 31) - 1, Nn=1 << 30, ldo=1 << 30) == N.NV_ERR_UNSUPPORTED
 
 
 def test_append_refusals():
@@ -165,3 +161,62 @@ def test_wrappers_take_device_tensors_only():
                  lambda: P.nv_op_attention_kv8(x[None], pages, i[None], i, 1.0)):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+# ---------------------------------------------------------------------- the rules, on their own
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("ops8")
+    src, out = str(d / "rule.cpp"), str(d / "rule.so")
+    with open(src, "w") as f:
+        f.write('''
+#include "linear8.h"
+extern "C" int form(long long M, int N, int K) { return nv::linear8_form(M, N, K); }
+extern "C" int forms() { return nv::L8_COUNT; }
+''')
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                        "paper_2312_04429_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", csrc,
+                    src, "-o", out], check=True)
+    lib = C.CDLL(out)
+    lib.form.argtypes = [C.c_longlong, C.c_int, C.c_int]
+    return lib
+
+
+def test_every_form_of_the_product_is_reached(rules):
+    assert sorted(FORM_SIZES) == list(range(rules.forms()))
+    for form, sizes in FORM_SIZES.items():
+        for s in sizes:
+            assert rules.form(*s) == form, s
+
+
+# us of each form (0 .. 7 as in linear8.h; None: not taken or not timed), graph-timed on one MI355X
+TIMINGS = [
+    (8, 1280, 5120, [7.3, 7.4, 10.7, 11.3, 13.9, 19.9, 19.0, None]),
+    (16, 320, 5120, [8.7, 7.4, 10.6, 11.4, 13.8, 19.6, 18.9, None]),
+    (16, 10240, 1280, [8.5, 9.5, 5.8, 6.1, 6.9, 9.2, 8.7, None]),
+    (32, 1280, 5120, [None, 7.5, 10.9, 11.5, 14.1, 20.1, 18.8, None]),
+    (64, 640, 640, [None, 5.9, 4.9, 5.1, 6.0, 8.1, 6.9, None]),
+    (128, 5120, 1280, [None, 13.6, 7.5, 6.4, 7.7, 10.6, 9.2, None]),
+    (256, 1280, 5120, [None, 16.4, 12.1, 13.5, 18.5, 33.6, 21.2, None]),
+    (256, 10240, 640, [None, 37.5, 11.6, 10.0, 8.6, 9.3, 8.2, None]),
+    (512, 2560, 2560, [None, 27.4, 13.1, 12.8, 12.1, 20.5, 14.9, None]),
+    (512, 5120, 640, [None, 37.9, 11.5, 10.1, 8.8, 9.3, 8.2, None]),
+    (1024, 1280, 1280, [None, 21.8, 8.5, 8.3, 8.4, 10.7, 9.4, 24.2]),
+    (1024, 5120, 1280, [None, 82.3, 26.8, 20.8, 18.0, 16.2, 19.6, 26.6]),
+    (2000, 1280, 5120, [None, 69.5, 37.2, 30.4, 28.2, 34.5, 22.9, 57.5]),
+    (2000, 2560, 1280, [None, 84.3, 26.8, 21.2, 17.9, 16.3, 19.3, 26.2]),
+    (4096, 1280, 1280, [None, 84.8, 26.8, 20.6, 18.2, 16.5, 20.1, 26.3]),
+    (4096, 5120, 640, [None, 294.9, 67.6, 50.6, 36.4, 31.3, 34.7, 39.4]),
+    (4096, 10240, 1280, [None, 657.6, 164.2, 131.3, 94.3, 75.2, 94.0, 78.6]),
+    (8192, 640, 2560, [None, 104.0, 39.0, 28.7, 25.2, 23.1, 28.3, 36.6]),
+    (8192, 2560, 2560, [None, 405.7, 128.9, 101.4, 80.6, 67.4, 76.3, 73.6]),
+    (8192, 10240, 5120, [None, 2229.4, 851.1, 704.2, 585.5, 428.5, 496.5, 363.1]),
+]
+
+
+@pytest.mark.parametrize("M,N,K,us", TIMINGS)
+def test_choice_of_form_is_near_the_fastest(M, N, K, us, rules):
+    pick = us[rules.form(M, N, K)]
+    assert pick is not None and pick <= 1.19 * min(t for t in us if t)
