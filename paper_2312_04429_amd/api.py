@@ -554,40 +554,64 @@ def nv_op_attention(q, k, vt, heads, scale, L=None, vt_row=None, out=None):
 # ---------------------------------------------------------------------- the 8-bit path
 
 _DT = {torch.float32: N.NV_F32, torch.float16: N.NV_F16, torch.bfloat16: N.NV_BF16}
-_CODES = (torch.float8_e4m3fn, torch.uint8)
-_SCALES = (torch.float8_e8m0fnu, torch.uint8)
+_HALF = frozenset((torch.float16, torch.bfloat16))
+_F32, _I32 = frozenset((torch.float32,)), frozenset((torch.int32,))
+_CODES = frozenset((torch.float8_e4m3fn, torch.uint8))
+_SCALES = frozenset((torch.float8_e8m0fnu, torch.uint8))
+
+# These calls take a few microseconds on the device, so the checks keep to a few hundred
+# nanoseconds a tensor: integers instead of device objects, addresses as plain integers.
 
 
-def _want(t, what, dtypes, shape=None, like=None):
-    """t is a device tensor of one of dtypes (and of `shape`, on like's device)."""
-    if not t.is_cuda or (like is not None and t.device != like.device):
-        raise ValueError(f"{what}: a tensor on {like.device if like is not None else 'a device'} "
-                         f"expected, got one on {t.device}")
+def _dev(t, what):
+    """The index of the device that a call's first tensor is on."""
+    d = t.get_device()
+    if d < 0:
+        raise ValueError(f"{what}: device tensor expected")
+    return d
+
+
+def _want(t, what, dtypes, dev, shape=None, flat=False):
+    """t is a tensor on device dev, of one of dtypes, of `shape`, contiguous if flat."""
+    if t.get_device() == dev and t.dtype in dtypes and (shape is None or t.shape == shape) and \
+            (not flat or t.is_contiguous()):
+        return
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: a tensor on device {dev} expected, got one on {t.device}")
     if t.dtype not in dtypes:
-        raise ValueError(f"{what}: dtype {t.dtype} not among {dtypes}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    raise ValueError(f"{what}: contiguous tensor expected")
 
 
 def _ld(t, what):
     """Row stride of a matrix whose rows are contiguous."""
     if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: a matrix of contiguous rows expected")
-    return max(t.stride(0), t.shape[1]) if t.shape[0] < 2 else t.stride(0)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
-def _flat(t, what):
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous tensor expected")
+def _call(name, dev, *args):
+    """A C entry point on device dev and its current stream (the last argument)."""
+    f = getattr(N.lib, name)
+    if dev == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if st != N.NV_OK:
+        N.check(st, name)
 
 
-def _on(t):
-    """The tensor's device made current, so that the stream and the launch are its own."""
-    return torch.cuda.device(t.device)
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _alloc_codes(M, K, device):
     """Codes [M][K] in rows of a multiple of 16 bytes (what nv_op_linear8 reads)."""
+    if K % 16 == 0:
+        return torch.empty((M, K), dtype=torch.float8_e4m3fn, device=device)
     return torch.empty((M, -(-K // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :K]
 
 
@@ -595,100 +619,82 @@ def nv_op_quant8(x, block_rows=1):
     """x [M][K] (float32, float16, bfloat16) in 8-bit form: e4m3 codes [M][K] and one
     power-of-two scale (float8_e8m0fnu) per 128 columns of a row (block_rows=1) or of 128
     rows (block_rows=128)."""
-    _want(x, "x", _DT)
-    ld = _ld(x, "x")
+    dev, ld = _dev(x, "x"), _ld(x, "x")
+    _want(x, "x", _DT, dev)
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows must be 1 or 128")
     M, K = x.shape
     q = _alloc_codes(M, K, x.device)
-    s = torch.empty((-(-M // block_rows) if block_rows in (1, 128) else 0, -(-K // 128)),
-                    dtype=torch.float8_e8m0fnu, device=x.device)
-    with _on(x):
-        st = N.lib.nv_op_quant8(_p(x), _DT[x.dtype], ld, M, K, block_rows, _p(q), q.stride(0),
-                                _p(s), _stream())
-    N.check(st, "nv_op_quant8")
+    s = torch.empty((-(-M // block_rows), -(-K // 128)), dtype=torch.float8_e8m0fnu,
+                    device=x.device)
+    _call("nv_op_quant8", dev, x.data_ptr(), _DT[x.dtype], ld, M, K, block_rows, q.data_ptr(),
+          q.stride(0), s.data_ptr())
     return q, s
-
-
-def _scales_ok(s, what, M, K, block_rows, like):
-    _want(s, what, _SCALES, (-(-M // block_rows), -(-K // 128)), like)
-    _flat(s, what)
 
 
 def nv_op_dequant8(q, scales, block_rows=1, dtype=torch.float16):
     """The values of an 8-bit matrix (nv_op_quant8, nv_op_rmsnorm8) as `dtype`."""
-    _want(q, "q", _CODES)
-    ld = _ld(q, "q")
+    dev, ld = _dev(q, "q"), _ld(q, "q")
+    _want(q, "q", _CODES, dev)
     M, K = q.shape
     if block_rows not in (1, 128) or dtype not in _DT:
         raise ValueError("block_rows must be 1 or 128, dtype float32, float16 or bfloat16")
-    _scales_ok(scales, "scales", M, K, block_rows, q)
+    _want(scales, "scales", _SCALES, dev, (-(-M // block_rows), -(-K // 128)), True)
     out = torch.empty((M, K), dtype=dtype, device=q.device)
-    with _on(q):
-        st = N.lib.nv_op_dequant8(_p(q), ld, _p(scales), M, K, block_rows, _p(out), _DT[dtype], K,
-                                  _stream())
-    N.check(st, "nv_op_dequant8")
+    _call("nv_op_dequant8", dev, q.data_ptr(), ld, scales.data_ptr(), M, K, block_rows,
+          out.data_ptr(), _DT[dtype], K)
     return out
 
 
 def nv_op_rmsnorm8(x, weight, residual=None, eps=1e-6):
     """(codes, scales, h) of weight * s / sqrt(mean(s^2) + eps), s = x + residual, for x [M][D]
     (float16, bfloat16) and weight [D] float32; h is s in x's type (None without a residual)."""
-    _want(x, "x", (torch.float16, torch.bfloat16))
-    ld = _ld(x, "x")
+    dev, ld = _dev(x, "x"), _ld(x, "x")
+    _want(x, "x", _HALF, dev)
     M, D = x.shape
-    _want(weight, "weight", (torch.float32,), (D,), x)
-    _flat(weight, "weight")
+    _want(weight, "weight", _F32, dev, (D,), True)
     h, ldr = None, 0
     if residual is not None:
-        _want(residual, "residual", (x.dtype,), (M, D), x)
+        _want(residual, "residual", (x.dtype,), dev, (M, D))
         ldr = _ld(residual, "residual")
         h = torch.empty((M, D), dtype=x.dtype, device=x.device)
     q = _alloc_codes(M, D, x.device)
     s = torch.empty((M, -(-D // 128)), dtype=torch.float8_e8m0fnu, device=x.device)
-    with _on(x):
-        st = N.lib.nv_op_rmsnorm8(_p(x), ld, _p(residual), ldr, _DT[x.dtype], _p(weight),
-                                  float(eps), M, D, _p(h), D, _p(q), q.stride(0), _p(s), _stream())
-    N.check(st, "nv_op_rmsnorm8")
+    _call("nv_op_rmsnorm8", dev, x.data_ptr(), ld, _at(residual), ldr, _DT[x.dtype],
+          weight.data_ptr(), eps, M, D, _at(h), D, q.data_ptr(), q.stride(0), s.data_ptr())
     return q, s, h
-
-
-def _ws_of(need, device, ws):
-    """(owner, address, bytes) of a workspace: the caller's, or one for this call."""
-    if ws is not None:
-        return ws
-    if need == 0:
-        return None, None, 0
-    own, addr = workspace(need, device)
-    return own, addr, need
 
 
 def nv_op_linear8(x, xs, w, ws, bias=None, residual=None, dtype=torch.float16, out=None):
     """out[M][N] = x[M][K] w[N][K]^T (+ bias) (+ residual) of 8-bit matrices: x with scales xs per
     128 columns of a row, w with scales ws per 128 x 128 (nv_op_quant8); bias float32, residual
     and out of `dtype`."""
-    _want(x, "x", _CODES)
-    _want(w, "w", _CODES, None, x)
-    ldx, ldw = _ld(x, "x"), _ld(w, "w")
+    dev, ldx, ldw = _dev(x, "x"), _ld(x, "x"), _ld(w, "w")
+    _want(x, "x", _CODES, dev)
+    _want(w, "w", _CODES, dev)
     (M, K), Nn = x.shape, w.shape[0]
-    if dtype not in (torch.float16, torch.bfloat16) or w.shape[1] != K:
+    if dtype not in _HALF or w.shape[1] != K:
         raise ValueError("dtype must be float16 or bfloat16, and w [N][K] have x's K columns")
-    _scales_ok(xs, "xs", M, K, 1, x)
-    _scales_ok(ws, "ws", Nn, K, 128, x)
+    KB = -(-K // 128)
+    _want(xs, "xs", _SCALES, dev, (M, KB), True)
+    _want(ws, "ws", _SCALES, dev, (-(-Nn // 128), KB), True)
     if bias is not None:
-        _want(bias, "bias", (torch.float32,), (Nn,), x)
-        _flat(bias, "bias")
+        _want(bias, "bias", _F32, dev, (Nn,), True)
     ldr = 0
     if residual is not None:
-        _want(residual, "residual", (dtype,), (M, Nn), x)
+        _want(residual, "residual", (dtype,), dev, (M, Nn))
         ldr = _ld(residual, "residual")
     if out is None:
-        out = torch.empty((M, Nn), dtype=dtype, device=x.device)
-    _want(out, "out", (dtype,), (M, Nn), x)
-    # a row of one may start at any stride, one that the kernel takes included
-    ldx, ldw = (-(-K // 16) * 16 if n < 2 else ld for ld, n in ((ldx, M), (ldw, Nn)))
-    with _on(x):
-        st = N.lib.nv_op_linear8(_p(x), ldx, _p(xs), _p(w), ldw, _p(ws), _p(bias), _p(residual),
-                                 ldr, _p(out), _ld(out, "out"), _DT[dtype], M, Nn, K, _stream())
-    N.check(st, "nv_op_linear8")
+        out, ldo = torch.empty((M, Nn), dtype=dtype, device=x.device), Nn
+    else:
+        _want(out, "out", (dtype,), dev, (M, Nn))
+        ldo = _ld(out, "out")
+    if M < 2:  # a single row starts at any stride, one that the kernel takes included
+        ldx = -(-K // 16) * 16
+    if Nn < 2:
+        ldw = -(-K // 16) * 16
+    _call("nv_op_linear8", dev, x.data_ptr(), ldx, xs.data_ptr(), w.data_ptr(), ldw, ws.data_ptr(),
+          _at(bias), _at(residual), ldr, out.data_ptr(), ldo, _DT[dtype], M, Nn, K)
     return out
 
 
@@ -702,24 +708,17 @@ def nv_kv8_pages(n_pages, heads, dh, device):
             z(n_pages, heads).view(torch.float8_e8m0fnu))
 
 
-def _pages(pages, like):
+def _pages(pages, dev):
     """Checks a cache and returns (kp, vp, ks, vs, n_pages, heads, dh)."""
     kp, vp, ks, vs = pages
-    _want(kp, "kp", _CODES, None, like)
     if kp.dim() != 4 or kp.shape[2] != N.NV_KV8_PAGE:
         raise ValueError("kp must be [n_pages][heads][64][dh]")
     n, h, _, dh = kp.shape
-    _want(vp, "vp", _CODES, (n, h, dh, N.NV_KV8_PAGE), like)
-    for t, what in ((ks, "ks"), (vs, "vs")):
-        _want(t, what, _SCALES, (n, h), like)
-    for t in pages:
-        _flat(t, "pages")
+    _want(kp, "kp", _CODES, dev, None, True)
+    _want(vp, "vp", _CODES, dev, (n, h, dh, N.NV_KV8_PAGE), True)
+    _want(ks, "ks", _SCALES, dev, (n, h), True)
+    _want(vs, "vs", _SCALES, dev, (n, h), True)
     return kp, vp, ks, vs, n, h, dh
-
-
-def _rows_of(t, what, rows, dtypes, like):
-    _want(t, what, dtypes, (rows,), like)
-    _flat(t, what)
 
 
 def _strides3(t, what):
@@ -729,72 +728,68 @@ def _strides3(t, what):
     return t.stride(1), t.stride(0)
 
 
+def _table(table, rows, dev):
+    if table.dim() != 2:
+        raise ValueError("table must be [rows][table_w]")
+    _want(table, "table", _I32, dev, (rows, table.shape[1]), True)
+    return table.shape[1]
+
+
 def nv_op_kv8_append(k, v, pages, table, pos, count=None):
     """Append tokens to an 8-bit cache in place: the first count[r] (None: all) of row r of
     k, v [rows][T][heads * dh] (float16, bfloat16) become tokens pos[r] .. of the sequence whose
     pages table[r] names (int32 [rows][table_w]; pos, count int32 [rows])."""
-    _want(k, "k", (torch.float16, torch.bfloat16))
-    kp, vp, ks, vs, n, H, dh = _pages(pages, k)
-    _want(v, "v", (k.dtype,), k.shape, k)
-    (ldk, kr), (ldv, vr) = _strides3(k, "k"), _strides3(v, "v")
+    dev, (ldk, kr), (ldv, vr) = _dev(k, "k"), _strides3(k, "k"), _strides3(v, "v")
+    _want(k, "k", _HALF, dev)
+    _want(v, "v", (k.dtype,), dev, k.shape)
+    kp, vp, ks, vs, n, H, dh = _pages(pages, dev)
     rows, T, cols = k.shape
     if cols != H * dh:
         raise ValueError(f"k and v need heads * dh = {H * dh} columns")
-    if table.dim() != 2:
-        raise ValueError("table must be [rows][table_w]")
-    _want(table, "table", (torch.int32,), (rows, table.shape[1]), k)
-    _flat(table, "table")
-    _rows_of(pos, "pos", rows, (torch.int32,), k)
+    W = _table(table, rows, dev)
+    _want(pos, "pos", _I32, dev, (rows,), True)
     if count is not None:
-        _rows_of(count, "count", rows, (torch.int32,), k)
-    with _on(k):
-        st = N.lib.nv_op_kv8_append(_p(k), ldk, kr, _p(v), ldv, vr, _DT[k.dtype], rows, T, H, dh,
-                                    _p(kp), _p(vp), _p(ks), _p(vs), n, _p(table), table.shape[1],
-                                    _p(pos), _p(count), _stream())
-    N.check(st, "nv_op_kv8_append")
+        _want(count, "count", _I32, dev, (rows,), True)
+    _call("nv_op_kv8_append", dev, k.data_ptr(), ldk, kr, v.data_ptr(), ldv, vr, _DT[k.dtype], rows,
+          T, H, dh, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, table.data_ptr(),
+          W, pos.data_ptr(), _at(count))
 
 
 def nv_op_attention_kv8_workspace(rows, S, heads, kv_heads, dh, table_w):
     return int(N.lib.nv_op_attention_kv8_workspace(rows, S, heads, kv_heads, dh, table_w))
 
 
-def nv_op_attention_kv8(q, pages, table, lens, scale, qpos=None, out=None, workspace=None):
+def nv_op_attention_kv8(q, pages, table, lens, scale, qpos=None, out=None, ws=None):
     """Multi-head attention of q [rows][S][heads * dh] (float16, bfloat16) over the first lens[r]
     cached tokens of each row; with qpos (int32 [rows]) query i of row r sees tokens up to
-    qpos[r] + i.  Query heads share the cache's heads in equal groups.  workspace: (owner,
-    address, bytes) of nv_op_attention_kv8_workspace(...) bytes, or None: one for this call."""
-    _want(q, "q", (torch.float16, torch.bfloat16))
-    kp, vp, ks, vs, n, H, dh = _pages(pages, q)
-    ldq, qr = _strides3(q, "q")
+    qpos[r] + i.  Query heads share the cache's heads in equal groups.  ws: (owner, address,
+    bytes) of nv_op_attention_kv8_workspace(...) bytes, or None: one for this call."""
+    dev, (ldq, qr) = _dev(q, "q"), _strides3(q, "q")
+    _want(q, "q", _HALF, dev)
+    kp, vp, ks, vs, n, H, dh = _pages(pages, dev)
     rows, S, cols = q.shape
     if cols == 0 or cols % (H * dh):
         raise ValueError(f"q needs a multiple of kv_heads * dh = {H * dh} columns")
-    if table.dim() != 2:
-        raise ValueError("table must be [rows][table_w]")
-    W = table.shape[1]
-    _want(table, "table", (torch.int32,), (rows, W), q)
-    _flat(table, "table")
-    _rows_of(lens, "lens", rows, (torch.int32,), q)
+    heads, W = cols // dh, _table(table, rows, dev)
+    _want(lens, "lens", _I32, dev, (rows,), True)
     if qpos is not None:
-        _rows_of(qpos, "qpos", rows, (torch.int32,), q)
+        _want(qpos, "qpos", _I32, dev, (rows,), True)
     if out is None:
-        out = torch.empty((rows, S, cols), dtype=q.dtype, device=q.device)
-    _want(out, "out", (q.dtype,), (rows, S, cols), q)
-    ldo, orow = _strides3(out, "out")
+        out, ldo, orow = torch.empty((rows, S, cols), dtype=q.dtype, device=q.device), cols, S * cols
+    else:
+        _want(out, "out", (q.dtype,), dev, (rows, S, cols))
+        ldo, orow = _strides3(out, "out")
     # strides of dimensions of one are free; any that the kernel takes will do
     if S < 2:
         ldq, ldo = cols, cols
     if rows < 2:
         qr, orow = 0, 0
-    heads = cols // dh
-    with _on(q):
-        need = nv_op_attention_kv8_workspace(rows, S, heads, H, dh, W)
-        _own, addr, need = _ws_of(need, q.device, workspace)
-        st = N.lib.nv_op_attention_kv8(_p(q), ldq, qr, _DT[q.dtype], _p(kp), _p(vp), _p(ks),
-                                       _p(vs), n, _p(table), W, _p(lens), _p(qpos), rows, S,
-                                       heads, H, dh, float(scale), _p(out), ldo, orow,
-                                       C.c_void_p(addr), need, _stream())
-    N.check(st, "nv_op_attention_kv8")
+    if ws is None:
+        need = N.lib.nv_op_attention_kv8_workspace(rows, S, heads, H, dh, W)
+        ws = workspace(need, q.device) + (need,) if need else (None, None, 0)
+    _call("nv_op_attention_kv8", dev, q.data_ptr(), ldq, qr, _DT[q.dtype], kp.data_ptr(),
+          vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, table.data_ptr(), W, lens.data_ptr(),
+          _at(qpos), rows, S, heads, H, dh, scale, out.data_ptr(), ldo, orow, ws[1], ws[2])
     return out
 
 

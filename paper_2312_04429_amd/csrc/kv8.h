@@ -23,20 +23,28 @@ struct Kv8AttnArgs {
   float scale;
   void* out;
   int64_t ldo, o_row;
-  int col_tiles, splits;
+  int col_tiles, splits, tall;
   float *part_o, *part_ml;    // per query and share: dh sums; (reference maximum, sum)
 };
 
 struct Kv8Plan {
-  int col_tiles;  // tiles of 16 queries of a kv head
+  int col_tiles;  // tiles of queries of a kv head
   int splits;     // shares of a row's pages
+  int tall;       // 0: tiles of 16 queries; 1, 2: of 64, 128 that share each page
 };
 
 inline Kv8Plan kv8_plan(int64_t rows, int S, int heads, int kv_heads, int table_w) {
-  const int64_t cols = (int64_t)S * (heads / kv_heads);
-  Kv8Plan p{(int)((cols + 15) / 16), 1};
-  const int64_t wgs = rows * kv_heads * p.col_tiles;
-  const int64_t want = std::max<int64_t>(1, 1024 / wgs), can = std::max(1, table_w / 8);
+  const int64_t cols = (int64_t)S * (heads / kv_heads), rh = rows * kv_heads;
+  if (cols > 32) {
+    const int tall = rh * ((cols + 127) / 128) > 256 ? 2 : 1;
+    Kv8Plan p{(int)((cols + 64 * tall - 1) / (64 * tall)), 1, tall};
+    const int64_t want = 512 / (rh * p.col_tiles), can = table_w / 4;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, can), 128));
+    return p;
+  }
+  Kv8Plan p{(int)((cols + 15) / 16), 1, 0};
+  const int64_t want = std::max<int64_t>(1, 1024 / (rh * p.col_tiles));
+  const int64_t can = std::max(1, table_w / 8);
   p.splits = (int)std::min<int64_t>(std::min(want, can), 256);
   return p;
 }

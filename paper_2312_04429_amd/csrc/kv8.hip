@@ -426,6 +426,341 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
   }
 }
 
+// Many queries of a head: four waves of QB * 16 queries share every page.  A page's codes come two
+// pages ahead into registers and are converted once, on their way into a double-buffered LDS
+// (16-bit: the products then read operands as they stand); key rows lie in the order in which
+// page_step takes them, so 16 rows are 16 consecutive ones.  A page that not every query sees whole
+// has its scores masked and its values behind the sequence zeroed; one with a NaN value among the
+// others waits until the loop is over and goes through page_step, which keeps it from the queries
+// that do not see it.  Workgroups run in
+// order of falling work under a causal limit: the last queries of every head first.
+template <typename T, int DH, int QB>
+__global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
+  using D = Dims<DH>;
+  using M = Mma<T>;
+  typedef typename M::Vec Vec;
+  constexpr int NW = 4, NT = NW * 64, COLS = NW * QB * 16;
+  constexpr int CW = DH % 16 ? 8 : 16;                       // codes of a key chunk
+  constexpr int KCH = DH / CW, KCN = PAGE * KCH, VCN = DH * 4;  // chunks of a page (values: 16 codes)
+  constexpr int KPT = (KCN + NT - 1) / NT, VPT = (VCN + NT - 1) / NT;
+  constexpr int KROW = (DH / 8) % 2 ? DH : DH + 8, VROW = PAGE + 8;  // odd counts of 16-byte chunks
+  constexpr int VR = D::DV * 16;
+  __shared__ __align__(16) T sk[2][PAGE * KROW];
+  __shared__ __align__(16) T sv[2][VR * VROW];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ uint32_t nan_pages;  // bit i: page least / 64 + i waits (at most COLS / 64 + 2 pages)
+  const int rh = blockIdx.x % (a.rows * a.kv_heads);  // a multiple of 8: one XCD's L2 for a head
+  const int rest = blockIdx.x / (a.rows * a.kv_heads), split = rest / a.col_tiles;
+  const int ct = a.col_tiles - 1 - rest % a.col_tiles;
+  const int head = rh % a.kv_heads, row = rh / a.kv_heads;
+  const int group = a.heads / a.kv_heads, cols = a.S * group, c0 = ct * COLS;
+  const int len = (int)std::min<int64_t>(std::max(a.lens[row], 0), (int64_t)a.table_w * PAGE);
+  const int64_t q0 = a.qpos ? (int64_t)a.qpos[row] + 1 : len;  // tokens that query 0 sees
+  auto sees = [&](int c) {                                     // tokens that column c sees
+    c = std::min(c, cols - 1) / group;
+    return (int)std::max<int64_t>(0, std::min<int64_t>(len, a.qpos ? q0 + c : len));
+  };
+  const int32_t* table = a.table + (int64_t)row * a.table_w;
+  const float scale2 = a.scale * LOG2E;
+
+  Vec fq[QB][D::STEPS];
+  State<DH> st[QB];
+  floatx4 sum[QB];  // of a lane's query, four times
+  int lim[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int col = std::min(c0 + (wave * QB + qb) * 16 + li, cols - 1);
+    lim[qb] = sees(col);
+    const T* qrow = (const T*)a.q + (int64_t)row * a.q_row + (int64_t)(col / group) * a.ldq +
+                    (int64_t)(head * group + col % group) * DH;
+#pragma unroll
+    for (int b = 0; b < D::STEPS; ++b) {
+      const int d = D::dim(b, kc);
+      fq[qb][b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
+    }
+    st[qb].m = -INFINITY, sum[qb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) st[qb].acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // the page at hand: its place, scales, and how its values enter the accumulators
+  struct Page { int64_t ph; int p, ke, ve; };
+  const int least = sees(c0), all = (sees(c0 + COLS - 1) + PAGE - 1) / PAGE;
+  const int pages = (int)((int64_t)all * (split + 1) / a.splits);  // the end of this share
+  const int wave_least = sees(c0 + wave * QB * 16), wave_most = sees(c0 + (wave + 1) * QB * 16 - 1);
+  // The next page that is there (p.ph < 0: none left).  Its table entry was read at the last call:
+  // the page's address does not wait for memory.
+  int pnext = (int)((int64_t)all * split / a.splits), entry = pnext < pages ? table[pnext] : 0;
+  auto take = [&](Page& p) {
+    p.ph = -1;
+    while (pnext < pages) {
+      const int64_t page = __builtin_amdgcn_readfirstlane(entry);
+      p.p = pnext++;
+      if (pnext < pages) entry = table[pnext];
+      if (page < 0 || page >= a.n_pages) continue;
+      p.ph = page * a.kv_heads + head;
+      p.ke = a.ks[p.ph], p.ve = a.vs[p.ph];
+      break;
+    }
+  };
+  struct Chunk { uint32_t w[CW / 4]; };
+  Chunk rk[KPT];
+  u32x4 rv[VPT];
+  auto fetch = [&](const Page& p) {
+    const uint8_t* kp = a.kp + p.ph * PAGE * DH;
+    const uint8_t* vp = a.vp + p.ph * PAGE * DH;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+      if (KCN % NT == 0 || tid + i * NT < KCN)
+        __builtin_memcpy(&rk[i], __builtin_assume_aligned(kp + (tid + i * NT) * CW, CW), CW);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (VCN % NT == 0 || tid + i * NT < VCN) rv[i] = *(const u32x4*)(vp + (tid + i * NT) * 16);
+  };
+  auto stash = [&](const Page& p, int buf, float vscale) {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      const int c = tid + i * NT, key = c / KCH;
+      if (KCN % NT != 0 && c >= KCN) break;
+      // key 16 g + 4 t + r goes to row 16 t + 4 g + r
+      T* to = sk[buf] + ((key >> 2 & 3) * 16 + (key >> 4) * 4 + (key & 3)) * KROW + c % KCH * CW;
+      *(Vec*)to = M::codes(rk[i].w[0], rk[i].w[1], 1.f);
+      if constexpr (CW == 16) *(Vec*)(to + 8) = M::codes(rk[i].w[2], rk[i].w[3], 1.f);
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int c = tid + i * NT;
+      if (VCN % NT != 0 && c >= VCN) break;
+      if (p.ve == 255) rv[i] = u32x4{0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F};
+      if (p.p * PAGE + PAGE > least) {  // uniform
+        rv[i] = keep_tokens(rv[i], len - p.p * PAGE - (c & 3) * 16);
+        if (nan_bytes(rv[i][0]) | nan_bytes(rv[i][1]) | nan_bytes(rv[i][2]) | nan_bytes(rv[i][3]))
+          atomicOr(&nan_pages, 1u << (p.p - least / PAGE));
+      }
+      T* to = sv[buf] + (c >> 2) * VROW + (c & 3) * 16;
+      *(Vec*)to = M::codes(rv[i][0], rv[i][1], vscale);
+      *(Vec*)(to + 8) = M::codes(rv[i][2], rv[i][3], vscale);
+    }
+  };
+  if (DH % 16)  // channels past dh: zeros
+    for (int i = tid; i < 2 * (VR - DH) * VROW; i += NT)
+      sv[i / ((VR - DH) * VROW)][DH * VROW + i % ((VR - DH) * VROW)] = (T)0.f;
+
+  // Unit of the accumulators, the same in every wave.  A page's exponent beside it is folded into
+  // its converted values where that is exact; one far above becomes the unit; for one far below the
+  // accumulators are brought to its size and back (exact too: they stay far from float32's ends; an
+  // exponent more than 80 below leaves the rest to the conversion, where float16 has no values and
+  // bfloat16 is exact for another 126).
+  int unit = 1;
+  struct How { float conv, pre, post; };  // factors of the values; of the accumulators, before, after
+  auto how = [&](const Page& p) {
+    const int d = p.ve == 255 ? 0 : p.ve - unit;
+    How h{1.f, 1.f, 1.f};
+    if (d > UNIT_HI) {
+      h.pre = ldexpf(1.f, -d), unit = p.ve;
+    } else if (d < UNIT_LO) {
+      const int e = std::max(d, -80);
+      h.pre = ldexpf(1.f, -e), h.post = ldexpf(1.f, e), h.conv = ldexpf(1.f, std::max(d - e, -126));
+    } else {
+      h.conv = __int_as_float((127 + d) << 23);
+    }
+    return h;
+  };
+
+  auto attend = [&](const Page& p, int buf, int j0, bool some) {
+    const T* K_ = sk[buf];
+    const T* V_ = sv[buf];
+    const float f = scale2 * scale_value(p.ke);
+    // Key fragments are requested TG tiles at a time, VG tiles of values before the softmax, whose
+    // arithmetic covers their way (left to itself the compiler reads each just before its
+    // multiply, and a SIMD has two waves to fill the wait with): all of them where 256 registers
+    // hold them.
+    constexpr int TG = DH >= 128 ? 2 : 4, VG = DH >= 128 ? D::DV / 2 : D::DV;
+    floatx4 s[QB][4];
+#pragma unroll
+    for (int t0 = 0; t0 < 4; t0 += TG) {
+      Vec fk[TG][D::STEPS];
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int b = 0; b < D::STEPS; ++b) {
+          const int d = D::dim(b, kc);  // past dh: the row's first codes against zeros
+          fk[t][b] = *(const Vec*)(K_ + ((t0 + t) * 16 + li) * KROW + (d < DH ? d : 0));
+        }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int b = 0; b < D::STEPS; ++b)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            s[qb][t0 + t] =
+                M::mul(fk[t][b], fq[qb][b], b ? s[qb][t0 + t] : floatx4{0.f, 0.f, 0.f, 0.f});
+    }
+    const T* vr = V_ + li * VROW + kc * 16;
+    auto value = [&](int j, int h2) { return *(const Vec*)(vr + j * 16 * VROW + h2 * 8); };
+    Vec fv[VG][2];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < VG; ++j) fv[j][0] = value(j, 0), fv[j][1] = value(j, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // scores relative to the query's reference; it moves only when one passes it by 2^8 (p stays
+    // below 256, as exact in 16 bits as below 1)
+    constexpr float MOVE = 8.f;
+    bool grow = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const float base = st[qb].m == -INFINITY ? 0.f : st[qb].m;
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[qb][t][r] = fmaf(s[qb][t][r], f, -base);
+          top = fmaxf(top, s[qb][t][r]);
+        }
+      if (some) {  // uniform
+        const int n = lim[qb] - j0 - 16 * kc;
+        top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (4 * t + r >= n) s[qb][t][r] = -INFINITY;
+            top = fmaxf(top, s[qb][t][r]);
+          }
+      }
+      grow |= !(top <= MOVE) || st[qb].m == -INFINITY;
+    }
+    if (__ballot(grow)) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[qb][t][r]);
+        top = rows_max(top);
+        const bool fresh = st[qb].m == -INFINITY;
+        const float move = fresh ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
+        const float mnew = fresh ? top : st[qb].m + move;
+        const float alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-move);
+        st[qb].m = mnew;
+        sum[qb] *= alpha;
+#pragma unroll
+        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= alpha;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[qb][t] -= move;
+      }
+    }
+    // the sums of the probabilities (as rounded) come out of the matrix unit, too: a row of ones
+    Vec fp[QB][2], ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (T)1.f;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          fp[qb][t >> 1][(t & 1) * 4 + r] = (T)__builtin_amdgcn_exp2f(s[qb][t][r]);
+      sum[qb] = M::mul(ones, fp[qb][0], sum[qb]);
+      sum[qb] = M::mul(ones, fp[qb][1], sum[qb]);
+    }
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) {
+      const Vec v0 = j < VG ? fv[j < VG ? j : 0][0] : value(j, 0);
+      const Vec v1 = j < VG ? fv[j < VG ? j : 0][1] : value(j, 1);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = M::mul(v0, fp[qb][0], st[qb].acc[j]);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = M::mul(v1, fp[qb][1], st[qb].acc[j]);
+    }
+  };
+
+  auto multiply = [&](const Page& p, const How& h, int buf) {
+    const int j0 = p.p * PAGE;
+    const bool some = j0 + PAGE > wave_least;  // some query of the wave sees part of it
+    if (h.pre != 1.f) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= h.pre;
+    }
+    if (j0 < wave_most && !(j0 + PAGE > least && (nan_pages >> (p.p - least / PAGE) & 1)))
+      attend(p, buf, j0, some);
+    if (h.post != 1.f) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= h.post;
+    }
+  };
+
+  Page cur, ahead;
+  How hc{1.f, 1.f, 1.f};
+  if (tid == 0) nan_pages = 0;
+  __syncthreads();
+  take(cur);
+  if (cur.ph >= 0) {
+    fetch(cur);
+    hc = how(cur);
+    stash(cur, 0, hc.conv);
+    take(ahead);
+    if (ahead.ph >= 0) fetch(ahead);
+    int buf = 0;
+    while (true) {
+      __syncthreads();  // the page is in LDS; the other buffer is read no more
+      multiply(cur, hc, buf);
+      if (ahead.ph < 0) break;
+      hc = how(ahead);
+      stash(ahead, buf ^ 1, hc.conv);
+      cur = ahead;
+      take(ahead);
+      if (ahead.ph >= 0) fetch(ahead);
+      buf ^= 1;
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    st[qb].unit = unit;
+    st[qb].l = kc == 0 ? sum[qb][0] : 0.f;
+    for (int p = least / PAGE; p < pages; ++p) {
+      if (!(nan_pages >> (p - least / PAGE) & 1)) continue;
+      const int64_t ph = (int64_t)table[p] * a.kv_heads + head;  // there: its codes were read
+      page_step<T, DH>(st[qb], fq[qb], a.kp + ph * PAGE * DH, a.vp + ph * PAGE * DH, a.ks[ph],
+                       a.vs[ph], scale2, p * PAGE, lim[qb], len, true, li, kc);
+    }
+    const float us = scale_value(st[qb].unit);
+    const int col = c0 + (wave * QB + qb) * 16 + li;
+    const float l = rows_sum(st[qb].l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (col >= cols) continue;
+    if (a.splits > 1) {
+      const int64_t slot = ((int64_t)rh * cols + col) * a.splits + split;
+#pragma unroll
+      for (int j = 0; j < D::DV; ++j) {
+        const int d = j * 16 + kc * 4;
+        if (DH % 16 == 0 || d < DH) *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * us;
+      }
+      if (kc == 0) a.part_ml[slot * 2] = st[qb].m, a.part_ml[slot * 2 + 1] = l;
+      continue;
+    }
+    T* to = (T*)a.out + (int64_t)row * a.o_row + (int64_t)(col / group) * a.ldo +
+            (int64_t)(head * group + col % group) * DH;
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) {
+      const int d = j * 16 + kc * 4;
+      if (DH % 16 && d >= DH) continue;
+      struct alignas(8) Quad { T v[4]; } out;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)(st[qb].acc[j][r] * us * inv);
+      *(Quad*)(to + d) = out;
+    }
+  }
+}
+
 // Shares of a query's pages, in order: one thread per four channels.
 template <typename T>
 __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
@@ -458,7 +793,10 @@ __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
 template <typename T, int DH>
 hipError_t attn_go(const Kv8AttnArgs& a, hipStream_t s) {
   const int64_t wgs = (int64_t)a.rows * a.kv_heads * a.col_tiles * a.splits;
-  hipLaunchKernelGGL((attn_kv8_k<T, DH>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)wgs);
+  if (a.tall == 0) hipLaunchKernelGGL((attn_kv8_k<T, DH>), grid, dim3(256), 0, s, a);
+  else if (a.tall == 1) hipLaunchKernelGGL((attn_kv8_tall_k<T, DH, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attn_kv8_tall_k<T, DH, 2>), grid, dim3(256), 0, s, a);
   if (a.splits > 1) {
     const int64_t n = (int64_t)a.rows * a.heads * a.S * (DH / 4);
     hipLaunchKernelGGL(attn_kv8_join_k<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 20)),
@@ -586,7 +924,7 @@ extern "C" int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row
   a.n_pages = n_pages, a.table = table, a.table_w = table_w, a.lens = lens, a.qpos = qpos;
   a.rows = rows, a.S = S, a.heads = heads, a.kv_heads = kv_heads, a.dh = dh, a.scale = scale;
   a.out = out, a.ldo = ldo, a.o_row = o_row_stride;
-  a.col_tiles = p.col_tiles, a.splits = p.splits;
+  a.col_tiles = p.col_tiles, a.splits = p.splits, a.tall = p.tall;
   if (need) {
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((uint8_t*)workspace + ml_at);
