@@ -582,7 +582,7 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
  *   token gets zeros.  Codes and scales of tokens that no query sees may hold
  *   anything, NaN among it.  float32 scores, softmax and sums; the
- *   probabilities enter the second product in dtype.  scale finite.
+ *   probabilities enter the second product in float16.  scale finite.
  *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV8_PAGE 64

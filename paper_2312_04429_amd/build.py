@@ -23,7 +23,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Wno-pass-failed"]
 
 
-# Per-source flags.  attention.hip: matrix instructions write VGPRs (its
+# Per-source flags.  attention.hip, kv8.hip: matrix instructions write VGPRs (their
 # softmax reads every score back; the accumulator-register form adds a copy
 # per score).  probe.hip: the same form, which is what reaches the matrix
 # cores' rate in a pure multiply loop (about 2.2 PFLOP/s against 1.2 with
@@ -31,6 +31,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # predictor.hip, ivf.hip: no multiply-add contraction, so their float64 sums
 # round exactly as written.
 EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "probe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "predictor.hip": ["-ffp-contract=off"],
          "ivf.hip": ["-ffp-contract=off"]}

@@ -3,9 +3,12 @@
 // Page: 64 tokens of one sequence.  Keys [head][64][dh] and values [head][dh][64] as e4m3
 // codes, one scale byte per page and head for each.
 //
-// Attention multiplies float16 (or bfloat16) matrices: codes convert exactly (three mantissa
-// bits), queries are taken as they are, and scales stay out of the 16-bit operands: a page's key
-// scale multiplies its scores in float32, its value scale the accumulators' common unit.
+// Attention multiplies 16-bit matrices: codes convert exactly (three mantissa bits), queries are
+// taken as they are, in their type, and scales stay out of the 16-bit operands: a page's key scale
+// multiplies its scores in float32, its value scale the accumulators' common unit.  The second
+// product is float16 for either type: probabilities of at most 256 lose 2^-11 there, 2^-8 in
+// bfloat16 (32 rows of up to 8192 tokens, bfloat16: error against float64 0.0022 -> 0.0017, of which
+// 0.0017 is the result's own rounding).
 // S^T = K Q^T is computed, so an accumulator entry's column is a query and the softmax state is a
 // lane's own; key row r of 16-key tile t is token 16 (r / 4) + 4 t + r % 4 of the page, so that
 // lane group kc ends up with tokens 16 kc .. 16 kc + 15: the probabilities are then the second
@@ -195,6 +198,14 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
 }
 
+// Pages p0 .. p1 - 1 of share `split` of a tile's pages: equal parts of at least KV8_SHARE pages, so a
+// short row's last shares may be empty.
+__device__ __forceinline__ void share_of(int pages, int split, int splits, int* p0, int* p1) {
+  const int n = std::max(KV8_SHARE, (pages + splits - 1) / splits);
+  *p0 = (int)std::min<int64_t>((int64_t)split * n, pages);
+  *p1 = std::min(*p0 + n, pages);
+}
+
 // One wave's running softmax over 16 queries: reference maximum, this lane's share of the sum,
 // accumulators O^T in units of 2^(unit - 127).
 template <int DH>
@@ -208,41 +219,69 @@ struct State {
 // 2^-5 .. 2^7 still normal float16 numbers.
 constexpr int UNIT_LO = -5, UNIT_HI = 7;
 
+// A lane's part of a page of one head: codes of keys 16 (li / 4) + 4 t + li % 4 and of 16 tokens of
+// channels 16 j + li, and the two scale bytes.
+template <int DH>
+struct PageCodes {
+  u32x4 k[4][Dims<DH>::FULL + 1];                              // [FULL]: not used
+  uint2 kr[4][Dims<DH>::STEPS - 2 * Dims<DH>::FULL + 1];       // [REST]: not used
+  u32x4 v[Dims<DH>::DV];
+  int ke, ve;
+  __device__ __forceinline__ void load_keys(const Kv8AttnArgs& a, int64_t ph, int li, int kc) {
+    using D = Dims<DH>;
+    const uint8_t* kp = a.kp + ph * PAGE * DH + (16 * (li >> 2) + (li & 3)) * DH;
+    ke = a.ks[ph];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int b = 0; b < D::FULL; ++b) k[t][b] = *(const u32x4*)(kp + 4 * t * DH + b * 64 + kc * 16);
+#pragma unroll
+      for (int b = 2 * D::FULL; b < D::STEPS; ++b) {
+        const int d = D::dim(b, kc);
+        kr[t][b - 2 * D::FULL] = d < DH ? *(const uint2*)(kp + 4 * t * DH + d) : make_uint2(0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void load_values(const Kv8AttnArgs& a, int64_t ph, int li, int kc) {
+    using D = Dims<DH>;
+    const uint8_t* vp = a.vp + ph * PAGE * DH + li * PAGE + kc * 16;
+    ve = a.vs[ph];
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j)
+      v[j] = DH % 16 == 0 || j * 16 + li < DH ? *(const u32x4*)(vp + j * 16 * PAGE)
+                                              : u32x4{0, 0, 0, 0};
+  }
+};
+
 // A page's 64 tokens, from token j0 of the sequence, into the state.  lim: tokens this lane's
 // query sees; len: tokens of the sequence; some: whether some query sees only part of them.
-template <typename T, int DH>
+// keys_done runs once the keys' registers are free again.
+template <typename T, int DH, typename Done>
 __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::Vec* fq,
-                                          const uint8_t* kp, const uint8_t* vp, int ke, int ve,
-                                          float scale2, int j0, int lim, int len, bool some,
-                                          int li, int kc) {
+                                          PageCodes<DH>& pc, float scale2, int j0, int lim, int len,
+                                          bool some, int kc, Done&& keys_done) {
   using D = Dims<DH>;
   using M = Mma<T>;
-  typedef typename M::Vec Vec;
+  using V = Mma<_Float16>;
+  u32x4(&v)[D::DV] = pc.v;
+  const int ke = __builtin_amdgcn_readfirstlane(pc.ke);
+  int ve = __builtin_amdgcn_readfirstlane(pc.ve);
   floatx4 s[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const uint8_t* kr = kp + (16 * (li >> 2) + 4 * t + (li & 3)) * DH;
     s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int b = 0; b < D::FULL; ++b) {
-      const u32x4 w = *(const u32x4*)(kr + b * 64 + kc * 16);
-      s[t] = M::mul(M::codes(w[0], w[1], 1.f), fq[2 * b], s[t]);
-      s[t] = M::mul(M::codes(w[2], w[3], 1.f), fq[2 * b + 1], s[t]);
+      s[t] = M::mul(M::codes(pc.k[t][b][0], pc.k[t][b][1], 1.f), fq[2 * b], s[t]);
+      s[t] = M::mul(M::codes(pc.k[t][b][2], pc.k[t][b][3], 1.f), fq[2 * b + 1], s[t]);
     }
 #pragma unroll
     for (int b = 2 * D::FULL; b < D::STEPS; ++b) {
-      const int d = D::dim(b, kc);
-      uint2 w = make_uint2(0, 0);
-      if (d < DH) w = *(const uint2*)(kr + d);
+      const uint2 w = pc.kr[t][b - 2 * D::FULL];
       s[t] = M::mul(M::codes(w.x, w.y, 1.f), fq[b], s[t]);
     }
   }
-  u32x4 v[D::DV];
-#pragma unroll
-  for (int j = 0; j < D::DV; ++j) {
-    const int c = j * 16 + li;
-    v[j] = DH % 16 == 0 || c < DH ? *(const u32x4*)(vp + c * PAGE + kc * 16) : u32x4{0, 0, 0, 0};
-  }
+  keys_done();
   const float f = scale2 * scale_value(ke);
   float top = -INFINITY;
 #pragma unroll
@@ -261,7 +300,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
     st.l *= alpha;
     st.m = mnew;
   }
-  Vec fp[2];
+  half8 fp[2];
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
@@ -269,7 +308,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
     for (int r = 0; r < 4; ++r) {
       const float p = __builtin_amdgcn_exp2f(s[t][r] - base);
       sum += p;
-      fp[t >> 1][(t & 1) * 4 + r] = (T)p;
+      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)p;
     }
   st.l += sum;
   if (ve == 255) {  // a NaN scale: every code of the page is NaN, the unit stays
@@ -289,12 +328,12 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
       for (int i = 0; i < 4; ++i) any |= nan_bytes(v[j][i]);
     }
     if (__ballot(any != 0)) {
-      Vec seen[2];
+      half8 seen[2];
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          seen[t >> 1][(t & 1) * 4 + r] = (T)(j0 + 16 * kc + 4 * t + r < lim ? 1.f : 0.f);
+          seen[t >> 1][(t & 1) * 4 + r] = (_Float16)(j0 + 16 * kc + 4 * t + r < lim ? 1.f : 0.f);
 #pragma unroll
       for (int j = 0; j < D::DV; ++j) {
         u32x4 ind;
@@ -305,8 +344,8 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
           v[j][i] &= ~(n * 0xFF);
         }
         floatx4 hit = {0.f, 0.f, 0.f, 0.f};
-        hit = M::mul(M::codes(ind[0], ind[1], 1.f), seen[0], hit);
-        hit = M::mul(M::codes(ind[2], ind[3], 1.f), seen[1], hit);
+        hit = V::mul(V::codes(ind[0], ind[1], 1.f), seen[0], hit);
+        hit = V::mul(V::codes(ind[2], ind[3], 1.f), seen[1], hit);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (hit[r] > 0.f) st.acc[j][r] = __int_as_float(0x7FC00000);
@@ -319,8 +358,8 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) {
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
-      o = M::mul(M::codes(v[j][0], v[j][1], 1.f), fp[0], o);
-      o = M::mul(M::codes(v[j][2], v[j][3], 1.f), fp[1], o);
+      o = V::mul(V::codes(v[j][0], v[j][1], 1.f), fp[0], o);
+      o = V::mul(V::codes(v[j][2], v[j][3], 1.f), fp[1], o);
       st.acc[j] += o * g;
     }
     return;
@@ -335,12 +374,12 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
   const float g = __int_as_float((127 + d) << 23);
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) {
-    st.acc[j] = M::mul(M::codes(v[j][0], v[j][1], g), fp[0], st.acc[j]);
-    st.acc[j] = M::mul(M::codes(v[j][2], v[j][3], g), fp[1], st.acc[j]);
+    st.acc[j] = V::mul(V::codes(v[j][0], v[j][1], g), fp[0], st.acc[j]);
+    st.acc[j] = V::mul(V::codes(v[j][2], v[j][3], g), fp[1], st.acc[j]);
   }
 }
 
-// A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and a
+// A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
 // share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
 // than one share the sums go to the workspace and attn_kv8_join_k adds them in order.
 template <typename T, int DH>
@@ -367,9 +406,8 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
   };
   const int lim = sees(qs), least = sees(c0 / group);
   const int most = sees((std::min(c0 + 16, cols) - 1) / group);
-  const int pages = (most + PAGE - 1) / PAGE;
-  const int p0 = (int)((int64_t)pages * split / a.splits);
-  const int p1 = (int)((int64_t)pages * (split + 1) / a.splits);
+  int p0, p1;
+  share_of((most + PAGE - 1) / PAGE, split, a.splits, &p0, &p1);
 
   Vec fq[D::STEPS];
   const T* qrow = (const T*)a.q + (int64_t)row * a.q_row + (int64_t)qs * a.ldq + (int64_t)qh * DH;
@@ -383,12 +421,32 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) st.acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   const float scale2 = a.scale * LOG2E;
-  for (int p = p0 + wave; p < p1; p += NW) {
-    const int64_t page = a.table[(int64_t)row * a.table_w + p];
-    if (page < 0 || page >= a.n_pages) continue;
-    const int64_t ph = page * a.kv_heads + head;
-    page_step<T, DH>(st, fq, a.kp + ph * PAGE * DH, a.vp + ph * PAGE * DH, a.ks[ph], a.vs[ph],
-                     scale2, p * PAGE, lim, len, p * PAGE + PAGE > least, li, kc);
+  // The next page's keys are requested as soon as this one's are multiplied, its values after this
+  // one's, into the same registers; its table entry was read a page earlier.
+  const int32_t* table = a.table + (int64_t)row * a.table_w;
+  int pn = p0 + wave, entry = pn < p1 ? table[pn] : 0;
+  auto take = [&](int& p) {  // page and head of the next page that is there; -1: none left
+    while (pn < p1) {
+      p = pn;
+      const int64_t page = __builtin_amdgcn_readfirstlane(entry);
+      pn += NW;
+      if (pn < p1) entry = table[pn];
+      if (page >= 0 && page < a.n_pages) return page * a.kv_heads + head;
+    }
+    return (int64_t)-1;
+  };
+  PageCodes<DH> pc;
+  int p = 0;
+  int64_t ph = take(p);
+  if (ph >= 0) pc.load_keys(a, ph, li, kc), pc.load_values(a, ph, li, kc);
+  while (ph >= 0) {
+    const int j0 = p * PAGE;
+    const int64_t next = take(p);
+    page_step<T, DH>(st, fq, pc, scale2, j0, lim, len, j0 + PAGE > least, kc, [&] {
+      if (next >= 0) pc.load_keys(a, next, li, kc);
+    });
+    if (next >= 0) pc.load_values(a, next, li, kc);
+    ph = next;
   }
   // the waves' states, in wave order
   const float l = rows_sum(st.l), us = scale_value(st.unit);
@@ -420,7 +478,7 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
       *(Quad*)((T*)a.out + (int64_t)row * a.o_row + (int64_t)qi * a.ldo + (int64_t)h * DH + d) = out;
     } else {
       const int64_t slot = (((int64_t)row * a.kv_heads + head) * cols + c0 + c) * a.splits + split;
-      *(floatx4*)(a.part_o + slot * DH + d) = o;
+      if (m != -INFINITY || ls != 0.f) *(floatx4*)(a.part_o + slot * DH + d) = o;
       if (d == 0) a.part_ml[slot * 2] = m, a.part_ml[slot * 2 + 1] = ls;
     }
   }
@@ -439,6 +497,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   using D = Dims<DH>;
   using M = Mma<T>;
   typedef typename M::Vec Vec;
+  using V = Mma<_Float16>;
   constexpr int NW = 4, NT = NW * 64, COLS = NW * QB * 16;
   constexpr int CW = DH % 16 ? 8 : 16;                       // codes of a key chunk
   constexpr int KCH = DH / CW, KCN = PAGE * KCH, VCN = DH * 4;  // chunks of a page (values: 16 codes)
@@ -446,7 +505,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   constexpr int KROW = (DH / 8) % 2 ? DH : DH + 8, VROW = PAGE + 8;  // odd counts of 16-byte chunks
   constexpr int VR = D::DV * 16;
   __shared__ __align__(16) T sk[2][PAGE * KROW];
-  __shared__ __align__(16) T sv[2][VR * VROW];
+  __shared__ __align__(16) _Float16 sv[2][VR * VROW];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __shared__ uint32_t nan_pages;  // bit i: page least / 64 + i waits (at most COLS / 64 + 2 pages)
@@ -486,12 +545,13 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 
   // the page at hand: its place, scales, and how its values enter the accumulators
   struct Page { int64_t ph; int p, ke, ve; };
-  const int least = sees(c0), all = (sees(c0 + COLS - 1) + PAGE - 1) / PAGE;
-  const int pages = (int)((int64_t)all * (split + 1) / a.splits);  // the end of this share
+  const int least = sees(c0);
+  int pnext, pages;  // the next page of this share, and its end
+  share_of((sees(c0 + COLS - 1) + PAGE - 1) / PAGE, split, a.splits, &pnext, &pages);
   const int wave_least = sees(c0 + wave * QB * 16), wave_most = sees(c0 + (wave + 1) * QB * 16 - 1);
   // The next page that is there (p.ph < 0: none left).  Its table entry was read at the last call:
   // the page's address does not wait for memory.
-  int pnext = (int)((int64_t)all * split / a.splits), entry = pnext < pages ? table[pnext] : 0;
+  int entry = pnext < pages ? table[pnext] : 0;
   auto take = [&](Page& p) {
     p.ph = -1;
     while (pnext < pages) {
@@ -538,20 +598,20 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
         if (nan_bytes(rv[i][0]) | nan_bytes(rv[i][1]) | nan_bytes(rv[i][2]) | nan_bytes(rv[i][3]))
           atomicOr(&nan_pages, 1u << (p.p - least / PAGE));
       }
-      T* to = sv[buf] + (c >> 2) * VROW + (c & 3) * 16;
-      *(Vec*)to = M::codes(rv[i][0], rv[i][1], vscale);
-      *(Vec*)(to + 8) = M::codes(rv[i][2], rv[i][3], vscale);
+      _Float16* to = sv[buf] + (c >> 2) * VROW + (c & 3) * 16;
+      *(half8*)to = V::codes(rv[i][0], rv[i][1], vscale);
+      *(half8*)(to + 8) = V::codes(rv[i][2], rv[i][3], vscale);
     }
   };
   if (DH % 16)  // channels past dh: zeros
     for (int i = tid; i < 2 * (VR - DH) * VROW; i += NT)
-      sv[i / ((VR - DH) * VROW)][DH * VROW + i % ((VR - DH) * VROW)] = (T)0.f;
+      sv[i / ((VR - DH) * VROW)][DH * VROW + i % ((VR - DH) * VROW)] = (_Float16)0.f;
 
   // Unit of the accumulators, the same in every wave.  A page's exponent beside it is folded into
   // its converted values where that is exact; one far above becomes the unit; for one far below the
   // accumulators are brought to its size and back (exact too: they stay far from float32's ends; an
-  // exponent more than 80 below leaves the rest to the conversion, where float16 has no values and
-  // bfloat16 is exact for another 126).
+  // exponent more than 80 below leaves the rest to the conversion, and one more than 113 below
+  // counts for nothing).
   int unit = 1;
   struct How { float conv, pre, post; };  // factors of the values; of the accumulators, before, after
   auto how = [&](const Page& p) {
@@ -570,7 +630,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 
   auto attend = [&](const Page& p, int buf, int j0, bool some) {
     const T* K_ = sk[buf];
-    const T* V_ = sv[buf];
+    const _Float16* V_ = sv[buf];
     const float f = scale2 * scale_value(p.ke);
     // Key fragments are requested TG tiles at a time, VG tiles of values before the softmax, whose
     // arithmetic covers their way (left to itself the compiler reads each just before its
@@ -598,9 +658,9 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
             s[qb][t0 + t] =
                 M::mul(fk[t][b], fq[qb][b], b ? s[qb][t0 + t] : floatx4{0.f, 0.f, 0.f, 0.f});
     }
-    const T* vr = V_ + li * VROW + kc * 16;
-    auto value = [&](int j, int h2) { return *(const Vec*)(vr + j * 16 * VROW + h2 * 8); };
-    Vec fv[VG][2];
+    const _Float16* vr = V_ + li * VROW + kc * 16;
+    auto value = [&](int j, int h2) { return *(const half8*)(vr + j * 16 * VROW + h2 * 8); };
+    half8 fv[VG][2];
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < VG; ++j) fv[j][0] = value(j, 0), fv[j][1] = value(j, 1);
@@ -655,27 +715,27 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
       }
     }
     // the sums of the probabilities (as rounded) come out of the matrix unit, too: a row of ones
-    Vec fp[QB][2], ones;
+    half8 fp[QB][2], ones;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (T)1.f;
+    for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.f;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          fp[qb][t >> 1][(t & 1) * 4 + r] = (T)__builtin_amdgcn_exp2f(s[qb][t][r]);
-      sum[qb] = M::mul(ones, fp[qb][0], sum[qb]);
-      sum[qb] = M::mul(ones, fp[qb][1], sum[qb]);
+          fp[qb][t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[qb][t][r]);
+      sum[qb] = V::mul(ones, fp[qb][0], sum[qb]);
+      sum[qb] = V::mul(ones, fp[qb][1], sum[qb]);
     }
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) {
-      const Vec v0 = j < VG ? fv[j < VG ? j : 0][0] : value(j, 0);
-      const Vec v1 = j < VG ? fv[j < VG ? j : 0][1] : value(j, 1);
+      const half8 v0 = j < VG ? fv[j < VG ? j : 0][0] : value(j, 0);
+      const half8 v1 = j < VG ? fv[j < VG ? j : 0][1] : value(j, 1);
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = M::mul(v0, fp[qb][0], st[qb].acc[j]);
+      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = V::mul(v0, fp[qb][0], st[qb].acc[j]);
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = M::mul(v1, fp[qb][1], st[qb].acc[j]);
+      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = V::mul(v1, fp[qb][1], st[qb].acc[j]);
     }
   };
 
@@ -729,8 +789,10 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
     for (int p = least / PAGE; p < pages; ++p) {
       if (!(nan_pages >> (p - least / PAGE) & 1)) continue;
       const int64_t ph = (int64_t)table[p] * a.kv_heads + head;  // there: its codes were read
-      page_step<T, DH>(st[qb], fq[qb], a.kp + ph * PAGE * DH, a.vp + ph * PAGE * DH, a.ks[ph],
-                       a.vs[ph], scale2, p * PAGE, lim[qb], len, true, li, kc);
+      PageCodes<DH> pc;
+      pc.load_keys(a, ph, li, kc);
+      pc.load_values(a, ph, li, kc);
+      page_step<T, DH>(st[qb], fq[qb], pc, scale2, p * PAGE, lim[qb], len, true, kc, [] {});
     }
     const float us = scale_value(st[qb].unit);
     const int col = c0 + (wave * QB + qb) * 16 + li;
@@ -742,7 +804,8 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 #pragma unroll
       for (int j = 0; j < D::DV; ++j) {
         const int d = j * 16 + kc * 4;
-        if (DH % 16 == 0 || d < DH) *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * us;
+        if ((DH % 16 == 0 || d < DH) && (st[qb].m != -INFINITY || l != 0.f))
+          *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * us;
       }
       if (kc == 0) a.part_ml[slot * 2] = st[qb].m, a.part_ml[slot * 2 + 1] = l;
       continue;
@@ -761,9 +824,53 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   }
 }
 
-// Shares of a query's pages, in order: one thread per four channels.
+// The shares of a query's pages, in order.  A workgroup per query: the shares' factors first, then
+// GROUPS threads per four channels that take every GROUPS-th share and meet in LDS.  A share that
+// held nothing has no sums (its maximum is -inf, its sum 0).
 template <typename T>
 __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
+  __shared__ float fac[KV8_MAX_SPLITS];
+  __shared__ float red[4][2];
+  __shared__ __align__(16) floatx4 part[256];
+  const int tid = threadIdx.x, group = a.heads / a.kv_heads, nq = a.dh / 4, groups = 256 / nq;
+  const int cols = a.S * group;
+  const int64_t u = blockIdx.x, rh = u / cols;
+  const int c = (int)(u - rh * cols);
+  const float* ml = a.part_ml + u * a.splits * 2;
+  float m = -INFINITY, l = 0.f;
+  if (tid < a.splits) m = ml[tid * 2], l = ml[tid * 2 + 1];
+  float top = rows_max(row16_max(m));
+  if ((tid & 63) == 0) red[tid >> 6][0] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+  const float base = top == -INFINITY ? 0.f : top;
+  const float f = __builtin_amdgcn_exp2f(m - base);
+  if (tid < a.splits) fac[tid] = m == -INFINITY && l == 0.f ? -1.f : f;  // -1: no sums
+  const float ls = wave_sum(f * l);  // the same tree in every call
+  if ((tid & 63) == 0) red[tid >> 6][1] = ls;
+  __syncthreads();
+  const float sum = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
+  const int g = tid / nq, d = (tid - g * nq) * 4;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  if (g < groups)
+#pragma unroll 4
+    for (int s = g; s < a.splits; s += groups)
+      if (fac[s] != -1.f) o += fac[s] * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
+  part[tid] = o;
+  __syncthreads();
+  if (tid >= nq) return;
+  for (int i = 1; i < groups && i < a.splits; ++i) o += part[i * nq + tid];
+  const int64_t row = rh / a.kv_heads, h = rh % a.kv_heads * group + c % group;
+  struct alignas(8) Quad { T v[4]; } out;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+  *(Quad*)((T*)a.out + row * a.o_row + c / group * a.ldo + h * a.dh + d) = out;
+}
+
+// The same with few shares: one thread per four channels.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_kv8_join_few_k(Kv8AttnArgs a) {
   const int group = a.heads / a.kv_heads, nq = a.dh / 4;
   const int64_t cols = (int64_t)a.S * group, total = a.rows * a.kv_heads * cols * nq;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total;
@@ -771,14 +878,22 @@ __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
     const int64_t u = i / nq, rh = u / cols, c = u - rh * cols;
     const int d = (int)(i - u * nq) * 4;
     const float* ml = a.part_ml + u * a.splits * 2;
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[s * 2]);
-    const float base = m == -INFINITY ? 0.f : m;
+    float m[KV8_FEW], l[KV8_FEW];
+    float top = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < KV8_FEW; ++s) {
+      m[s] = s < a.splits ? ml[s * 2] : -INFINITY;
+      l[s] = s < a.splits ? ml[s * 2 + 1] : 0.f;
+      top = fmaxf(top, m[s]);
+    }
+    const float base = top == -INFINITY ? 0.f : top;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
     float ls = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-      const float f = __builtin_amdgcn_exp2f(ml[s * 2] - base);
-      ls += f * ml[s * 2 + 1];
+#pragma unroll
+    for (int s = 0; s < KV8_FEW; ++s) {
+      if (m[s] == -INFINITY && l[s] == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(m[s] - base);
+      ls += f * l[s];
       o += f * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
     }
     const int64_t row = rh / a.kv_heads, h = rh % a.kv_heads * group + c % group;
@@ -797,11 +912,13 @@ hipError_t attn_go(const Kv8AttnArgs& a, hipStream_t s) {
   if (a.tall == 0) hipLaunchKernelGGL((attn_kv8_k<T, DH>), grid, dim3(256), 0, s, a);
   else if (a.tall == 1) hipLaunchKernelGGL((attn_kv8_tall_k<T, DH, 1>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((attn_kv8_tall_k<T, DH, 2>), grid, dim3(256), 0, s, a);
-  if (a.splits > 1) {
-    const int64_t n = (int64_t)a.rows * a.heads * a.S * (DH / 4);
-    hipLaunchKernelGGL(attn_kv8_join_k<T>, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 20)),
+  const int64_t queries = (int64_t)a.rows * a.heads * a.S;
+  if (a.splits > KV8_FEW)
+    hipLaunchKernelGGL(attn_kv8_join_k<T>, dim3((unsigned)queries), dim3(256), 0, s, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL(attn_kv8_join_few_k<T>,
+                       dim3((unsigned)std::min<int64_t>(ceil_div(queries * (DH / 4), 256), 1 << 20)),
                        dim3(256), 0, s, a);
-  }
   return hipGetLastError();
 }
 

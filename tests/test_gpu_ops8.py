@@ -15,10 +15,10 @@ whole step: the matrix unit's own rounding of its sums is not specified to be to
               their sizes, one rounding u(t)
   attention   a score is dh float32 additions and three products: (dh E sum |q k| + 4 E |score|)
               absolute, the shift by the maximum and the exponential 4 E |score| + 4 E; twice that
-              (numerator and sum) is a probability's relative error; its rounding to t is u(t)
-              relative, or 2^-25 absolute where float16 is subnormal (256 times less than its
-              probability's unit, the reference maximum being the true one); sums of n terms in
-              float32: n E; all of sum p |v|, and one rounding u(t) of the result
+              (numerator and sum) is a probability's relative error; its rounding to float16 is
+              2^-11 relative, in numerator and sum, or 2^-25 absolute where it is subnormal (the
+              reference maximum is at most the true one); sums of n terms in float32: n E; all of
+              sum p |v|, and one rounding u(t) of the result
 """
 import numpy as np
 import pytest
@@ -380,8 +380,8 @@ def check_attention(q, pages, table, lens, scale, H, qpos=None, **kw):
     got = np64(out).reshape(o.shape)
     big = np.nanmax(np.abs(O.VALUES[pages[1]]), initial=0) * \
         2.0 ** (int(np.where(pages[3] < 255, pages[3], 0).max()) - 127.0)
-    rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + u(q.dtype) + n * E
-    tol = rel * spread * (1 + u(q.dtype)) + n * 2.0 ** -25 * (q.dtype == F16) * big \
+    rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + 2 * u(F16) + n * E
+    tol = rel * spread * (1 + u(q.dtype)) + n * 2.0 ** -25 * (big + np.abs(o)) \
         + u(q.dtype) * np.abs(o) + (2.0 ** -25 if q.dtype == F16 else 0)
     assert np.array_equal(np.isnan(got), np.isnan(o))
     with np.errstate(invalid="ignore"):
@@ -604,7 +604,7 @@ def test_layer_of_all_of_them(dtype):
             assert np.array_equal(bits(g), w)
         o, spread, size, most = O.attention(np64(qkv[:, :, :C]).reshape(R, n, Hq, dh), ok, ov, oks, ovs,
                                             tb, ps + cn, dh ** -0.5, H, ps)
-        rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + 2 * u(dtype) + W * 64 * E
+        rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + 2 * u(F16) + u(dtype) + W * 64 * E
         assert (np.abs(np64(a).reshape(o.shape) - o) <= rel * spread + 1e-5).all()
         assert not torch.isnan(h2).any() and not ((bits(q2) & 127) == 127).any()
         # the whole step against float64 products of the same 8-bit operands: the first norm's
