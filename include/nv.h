@@ -512,10 +512,10 @@ int32_t nv_op_attention(const void* q, const void* k, const void* vt, void* out,
  * even, and elements that are not finite become NaN.
  *
  * Sizes of zero (M, rows, S, T) are legal and launch nothing.  Strides are in
- * elements (bytes for 8-bit rows).  Buffers that are not 16-byte aligned, or
- * rows whose stride or length does not keep 8 elements together, are taken
- * element by element (nv_op_linear8's operands: refused, see there).  Inputs
- * and outputs may not overlap unless said.
+ * elements (bytes for 8-bit rows).  Rows may start at any element and have any
+ * length (but for nv_op_linear8's operands and nv_op_attention_kv8's queries
+ * and outputs, see there); 16-byte aligned ones are fastest.  Inputs and
+ * outputs may not overlap unless said.
  *
  * nv_op_quant8: x [M] rows of K (x_dtype NV_F32, NV_F16 or NV_BF16, ldx apart)
  *   into 8-bit form.  1 <= K.

@@ -13,7 +13,6 @@ struct Linear8Args {
   void* out;                        // [M][ldo]
   int64_t M;
   int N, K;
-  int vec;                          // four columns of out, residual and bias move as a vector
 };
 
 constexpr int S8_TILES = 48;  // 128-deep tiles whose scale bytes sit in LDS at a time

@@ -55,20 +55,25 @@ __device__ __forceinline__ void mask_tail(intx8& f, int left) {
   }
 }
 
-// bias, residual, rounding and store of columns n .. n + 3 of row m
+// bias, residual, rounding and store of columns n .. n + 3 of row m (those below N)
 template <typename T>
 __device__ __forceinline__ void store_quad(const Linear8Args& g, int64_t m, int n, floatx4 v) {
-  struct alignas(8) Quad { T v[4]; };
+  struct __attribute__((packed, aligned(sizeof(T)))) Quad { T v[4]; };
+  struct __attribute__((packed, aligned(4))) Quad32 { float v[4]; };
   T* o = (T*)g.out + m * g.ldo + n;
   const T* r = (const T*)g.residual + m * g.ldr + n;
-  if (g.vec && n + 4 <= g.N) {
-    if (g.bias) v += *(const floatx4*)(g.bias + n);
+  if (n + 4 <= g.N) {
+    if (g.bias) {
+      const Quad32 b = *(const Quad32*)(g.bias + n);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += b.v[i];
+    }
+    Quad q;
     if (g.residual) {
-      const Quad q = *(const Quad*)r;
+      q = *(const Quad*)r;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] += (float)q.v[i];
     }
-    Quad q;
 #pragma unroll
     for (int i = 0; i < 4; ++i) q.v[i] = (T)v[i];
     *(Quad*)o = q;
@@ -309,9 +314,13 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   float* mine = (float*)(ring + wave * (STAGES * TILE / NW));
   const float* first = (const float*)(smem + wave * (STAGES * TILE / NW));  // team 0's part
   const int c = lane % LPR * 2, n = n0 + wn * WN + c * 4;
-  const bool whole = g.vec && n + 8 <= g.N;
+  const bool whole = n + 8 <= g.N;
   floatx4 blo = {0.f, 0.f, 0.f, 0.f}, bhi = blo;
-  if (whole && g.bias) blo = *(const floatx4*)(g.bias + n), bhi = *(const floatx4*)(g.bias + n + 4);
+  if (whole && g.bias) {
+    const Any8<float> b = *(const Any8<float>*)(g.bias + n);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) blo[e] = b.v[e], bhi[e] = b.v[4 + e];
+  }
 #pragma unroll
   for (int i0 = 0; i0 < FM; i0 += IB) {
 #pragma unroll
@@ -338,16 +347,16 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
         }
       }
       if (whole) {
-        struct alignas(8) Eight { T v[8]; } q[U];  // 8 bytes apart is all that vec asks for
+        Any8<T> q[U];  // rows start anywhere: vectors aligned as their elements
         if (g.residual) {
 #pragma unroll
           for (int k = 0; k < U; ++k) {
             const int64_t m = std::min<int64_t>(mw + r0 + k * STEP, g.M - 1);
-            q[k] = *(const Eight*)((const T*)g.residual + m * g.ldr + n);
+            q[k] = *(const Any8<T>*)((const T*)g.residual + m * g.ldr + n);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < U; ++k) q[k] = Eight{};
+          for (int k = 0; k < U; ++k) q[k] = Any8<T>{};
         }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
@@ -357,7 +366,7 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
             q[k].v[e] = (T)(lo[k][e] + blo[e] + (float)q[k].v[e]);
             q[k].v[4 + e] = (T)(hi[k][e] + bhi[e] + (float)q[k].v[4 + e]);
           }
-          if (m < g.M) *(Eight*)((T*)g.out + m * g.ldo + n) = q[k];
+          if (m < g.M) *(Any8<T>*)((T*)g.out + m * g.ldo + n) = q[k];
         }
       } else {
 #pragma unroll
@@ -517,8 +526,6 @@ extern "C" int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, 
   g.ldx = ldx, g.ldw = ldw, g.ldr = ldr, g.ldo = ldo;
   g.bias = bias, g.residual = residual, g.out = out;
   g.M = M, g.N = N, g.K = K;
-  g.vec = ldo % 4 == 0 && (uintptr_t)out % 8 == 0 && (!bias || aligned16(bias)) &&
-          (!residual || (ldr % 4 == 0 && (uintptr_t)residual % 8 == 0));
   const hipStream_t s = (hipStream_t)stream;
   NV_HIP_TRY(dtype == NV_F16 ? launch<_Float16>(g, form, s) : launch<__bf16>(g, form, s));
   return NV_OK;
