@@ -6,7 +6,7 @@
 namespace nv {
 
 struct Kv8AppendArgs {
-  const uint8_t *k, *v;       // 16-bit elements
+  const void *k, *v;
   uint8_t *kp, *vp, *ks, *vs;
   int64_t ldk, k_row, ldv, v_row, n_pages;
   const int32_t *table, *pos, *count;

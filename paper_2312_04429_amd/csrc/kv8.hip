@@ -24,6 +24,7 @@ namespace nv {
 namespace {
 
 constexpr int PAGE = NV_KV8_PAGE;
+constexpr int KV8_FEW_TOKENS = 4;  // of a row, that a wave appends on its own
 constexpr float LOG2E = 1.4426950408889634f;
 
 // ------------------------------------------------------------------------------------ append
@@ -35,55 +36,142 @@ __device__ __forceinline__ uint32_t recode4(uint32_t w, float f) {
   return codes4(a[0], a[1], b[0], b[1], f);
 }
 
-// A workgroup per (row, touched page, head) and tensor: the new tokens' values stay in registers
-// between their largest magnitude and their codes.  Bound by latency for single tokens, by HBM
-// for prompts (the value codes are transposed in LDS and leave as 4-byte words).
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) kv8_append_k(Kv8AppendArgs a) {
-  constexpr int MAXU = 64 * 160 / 8 / 256;  // eights of new values a thread can hold
-  __shared__ float part[4];
-  __shared__ __align__(16) uint8_t tr[160 * 68];  // [channel][64 tokens], rows 68 bytes apart
-  const int tid = threadIdx.x, head = blockIdx.y >> 1;
-  const bool is_v = blockIdx.y & 1;
-  const int64_t row = blockIdx.z;
-  const int64_t pos = a.pos[row];
-  const int cnt = a.count ? std::min(std::max(a.count[row], 0), a.T) : a.T;
-  if (pos < 0) return;
-  const int64_t p = pos / PAGE + blockIdx.x, first = p * PAGE;
-  const int64_t lo = std::max(pos, first), hi = std::min(pos + cnt, first + PAGE);
-  if (lo >= hi || p >= a.table_w) return;
-  const int64_t page = a.table[row * a.table_w + p];
-  if (page < 0 || page >= a.n_pages) return;
-  const int t0 = (int)(lo - first), t1 = (int)(hi - first);  // new tokens of the page
-  const int dh = a.dh, nch = dh / 8, units = (t1 - t0) * nch;
-  const T* src = (const T*)(is_v ? a.v + row * a.v_row * sizeof(T) : a.k + row * a.k_row * sizeof(T));
-  const int64_t ld = is_v ? a.ldv : a.ldk;
-  src += (lo - pos) * ld + (int64_t)head * dh;
-  const int64_t ph = page * a.heads + head;
-  uint8_t* codes = (is_v ? a.vp : a.kp) + ph * PAGE * dh;
-  uint8_t* scale = (is_v ? a.vs : a.ks) + ph;
+// What a call appends to the slot-th page that a row's tokens touch: tokens t0 .. t1 - 1 of it, from
+// src on, ld apart.  False: nothing.
+template <typename T>
+struct Appended {
+  const T* src;
+  int64_t ld;
+  uint8_t *codes, *scale;
+  int t0, t1;
+  __device__ __forceinline__ bool find(const Kv8AppendArgs& a, int64_t row, int head, bool is_v,
+                                       int slot) {
+    const int64_t pos = a.pos[row];
+    const int cnt = a.count ? std::min(std::max(a.count[row], 0), a.T) : a.T;
+    if (pos < 0) return false;
+    const int64_t p = pos / PAGE + slot, first = p * PAGE;
+    const int64_t lo = std::max(pos, first), hi = std::min(pos + cnt, first + PAGE);
+    if (lo >= hi || p >= a.table_w) return false;
+    const int64_t page = a.table[row * a.table_w + p];
+    if (page < 0 || page >= a.n_pages) return false;
+    t0 = (int)(lo - first), t1 = (int)(hi - first);
+    ld = is_v ? a.ldv : a.ldk;
+    src = (const T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) + (lo - pos) * ld +
+          (int64_t)head * a.dh;
+    const int64_t ph = page * a.heads + head;
+    codes = (is_v ? a.vp : a.kp) + ph * PAGE * a.dh;
+    scale = (is_v ? a.vs : a.ks) + ph;
+    return true;
+  }
+};
 
+// Up to KV8_FEW_TOKENS tokens a row: a wave for what a workgroup does below.  Its lanes take eight
+// channels of a token each; nothing waits for a barrier, and 32 registers keep the chip full of
+// them (200 rows of one token, 8 heads of 128: 16.7 us with the
+// kernel below, 7.1 here; four rows of 1000 tokens are the other kernel's, 13 us).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) kv8_append_few_k(Kv8AppendArgs a, int64_t units, int slots) {
+  constexpr int MAXU = (KV8_FEW_TOKENS * 160 / 8 + 63) / 64;
+  const int lane = threadIdx.x & 63;
+  int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= units) return;
+  const bool is_v = id & 1;
+  id >>= 1;
+  const int head = (int)(id % a.heads);
+  id /= a.heads;
+  Appended<T> t;
+  if (!t.find(a, id / slots, head, is_v, (int)(id % slots))) return;
+  const int dh = a.dh, nch = dh / 8, n = (t.t1 - t.t0) * nch, t0 = t.t0;
+  const int old = t0 > 0 ? *t.scale : 0;
   float v[MAXU][8];
   float top = 0.f;
 #pragma unroll
   for (int u = 0; u < MAXU; ++u) {
-    const int i = u * 256 + tid;
-    if (u * 256 >= units) break;  // uniform
-    const int t = i / nch, c = (i - t * nch) * 8;
-    load8<VEC>(src + t * ld, c, i < units ? dh : 0, v[u]);
+    const int i = u * 64 + lane, k = i / nch;
+    load8<VEC>(t.src + k * t.ld, (i - k * nch) * 8, i < n ? dh : 0, v[u]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[u][j]));
   }
-  top = rows_max(row16_max(top));
-  if ((tid & 63) == 0) part[tid >> 6] = top;
-  const int old = t0 > 0 ? *scale : 0;
-  __syncthreads();  // the old scale has been read, too
-  const int e = std::max(old, scale_byte(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]))));
+  const int e = std::max(old, scale_byte(rows_max(row16_max(top))));
   const float inv = ldexpf(1.f, 127 - e), move = ldexpf(1.f, old - e);
-  const bool grow = t0 > 0 && e > old;
-  if (tid == 0 && (t0 == 0 || grow)) *scale = (uint8_t)e;
+  if (t0 > 0 && e > old) {  // the old codes to the larger scale
+    if (!is_v) {
+      for (int i = lane; i < t0 * nch; i += 64) {
+        uint2* w = (uint2*)(t.codes + i * 8);
+        *w = make_uint2(recode4(w->x, move), recode4(w->y, move));
+      }
+    } else {
+      const int nw = (t0 + 3) / 4;  // the last word of a channel may hold new tokens: single codes
+      for (int i = lane; i < dh * nw; i += 64) {
+        const int c = i / nw, b = (i - c * nw) * 4;
+        uint8_t* to = t.codes + c * PAGE + b;
+        const uint32_t w = recode4(*(const uint32_t*)to, move);
+        if (b + 4 <= t0) *(uint32_t*)to = w;
+        else
+          for (int k = 0; b + k < t0; ++k) to[k] = (uint8_t)(w >> (8 * k));
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < MAXU; ++u) {
+    const int i = u * 64 + lane, k = i / nch, c = (i - k * nch) * 8;
+    if (i >= n) continue;
+    if (!is_v) {
+      store_codes8<true>(t.codes + t0 * dh, i * 8, n * 8, v[u], inv);
+    } else {
+      const uint32_t w0 = codes4(v[u][0], v[u][1], v[u][2], v[u][3], inv);
+      const uint32_t w1 = codes4(v[u][4], v[u][5], v[u][6], v[u][7], inv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        t.codes[(c + j) * PAGE + t0 + k] = (uint8_t)((j < 4 ? w0 : w1) >> (8 * (j & 3)));
+    }
+  }
+  if (lane == 0 && (t0 == 0 || e > old)) *t.scale = (uint8_t)e;
+}
+
+__device__ __forceinline__ float block_max(float v, float* part) {
+  v = rows_max(row16_max(v));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+
+// A workgroup per (row, touched page, head) and tensor: the new tokens' values stay in registers
+// between their largest magnitude and their codes.  A thread takes eight channels of single tokens
+// for keys, and of four neighbouring tokens for values: their codes of one channel are a word of the
+// transposed page, sixteen lanes write a whole row of it, and nothing passes through LDS (through it,
+// byte by byte, 8 prompts of 2000 tokens, 8 heads of 128, took 28.8 us, so 23.6).  Bound by launch and
+// latency for single tokens, by HBM for prompts.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) kv8_append_k(Kv8AppendArgs a) {
+  __shared__ float part[4];
+  const int tid = threadIdx.x;
+  const bool is_v = blockIdx.y & 1;
+  Appended<T> at;
+  if (!at.find(a, blockIdx.z, blockIdx.y >> 1, is_v, blockIdx.x)) return;  // uniform
+  const int dh = a.dh, nch = dh / 8, t0 = at.t0, t1 = at.t1;
+  const T* src = at.src;
+  const int64_t ld = at.ld;
+  uint8_t *codes = at.codes, *scale = at.scale;
+  const int old = t0 > 0 ? *scale : 0;  // before block_max's barrier: thread 0 writes it after
+  float top = 0.f;
+  int e;
   if (!is_v) {
-    if (grow)
+    constexpr int MAXU = 64 * 160 / 8 / 256;
+    const int units = (t1 - t0) * nch;
+    float v[MAXU][8];
+#pragma unroll
+    for (int u = 0; u < MAXU; ++u) {
+      const int i = u * 256 + tid;
+      if (u * 256 >= units) break;  // uniform
+      const int t = i / nch, c = (i - t * nch) * 8;
+      load8<VEC>(src + t * ld, c, i < units ? dh : 0, v[u]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[u][j]));
+    }
+    e = std::max(old, scale_byte(block_max(top, part)));
+    const float inv = ldexpf(1.f, 127 - e), move = ldexpf(1.f, old - e);
+    if (t0 > 0 && e > old)
       for (int i = tid; i < t0 * nch; i += 256) {
         uint2* w = (uint2*)(codes + i * 8);
         *w = make_uint2(recode4(w->x, move), recode4(w->y, move));
@@ -94,42 +182,53 @@ __global__ void __launch_bounds__(256) kv8_append_k(Kv8AppendArgs a) {
       if (u * 256 >= units) break;
       if (i < units) store_codes8<true>(codes + t0 * dh, i * 8, units * 8, v[u], inv);
     }
-    return;
-  }
+  } else {
+    constexpr int MAXU = (16 * 160 / 8 + 255) / 256;
+    float v[MAXU][4][8];
 #pragma unroll
-  for (int u = 0; u < MAXU; ++u) {
-    const int i = u * 256 + tid;
-    if (u * 256 >= units) break;
-    const int t = i / nch, c = (i - t * nch) * 8;
-    if (i < units) {
-      const uint32_t w0 = codes4(v[u][0], v[u][1], v[u][2], v[u][3], inv);
-      const uint32_t w1 = codes4(v[u][4], v[u][5], v[u][6], v[u][7], inv);
+    for (int u = 0; u < MAXU; ++u) {
+      const int t = (tid & 15) * 4, c = (u * 16 + (tid >> 4)) * 8;  // c >= dh: no channels
+      if (u * 128 >= dh) break;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        tr[(c + j) * 68 + t0 + t] = (uint8_t)((j < 4 ? w0 : w1) >> (8 * (j & 3)));
-    }
-  }
-  __syncthreads();
-  // words of four tokens: new codes within [t0, t1), old ones (moved if the scale grew) before,
-  // what was there behind
-  const int w0 = (grow ? 0 : t0) / 4, nw = (t1 + 3) / 4 - w0;
-  for (int i = tid; i < dh * nw; i += 256) {
-    const int c = i / nw, t = (w0 + i - c * nw) * 4;
-    uint32_t* to = (uint32_t*)(codes + c * PAGE + t);
-    uint32_t fresh = *(const uint32_t*)(tr + c * 68 + t);
-    if (t < t0 || t + 4 > t1) {
-      const uint32_t was = *to;
-      const uint32_t kept = grow ? recode4(was, move) : was;
-      uint32_t w = 0;
+      for (int k = 0; k < 4; ++k) {
+        const bool there = c < dh && t + k >= t0 && t + k < t1;
+        load8<VEC>(src + (t + k - t0) * ld, c, there ? dh : 0, v[u][k]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t m = 0xFFu << (8 * j);
-        w |= (t + j < t0 ? kept : t + j < t1 ? fresh : was) & m;
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[u][k][j]));
       }
-      fresh = w;
     }
-    *to = fresh;
+    e = std::max(old, scale_byte(block_max(top, part)));
+    const float inv = ldexpf(1.f, 127 - e), move = ldexpf(1.f, old - e);
+    const bool grow = t0 > 0 && e > old;
+#pragma unroll
+    for (int u = 0; u < MAXU; ++u) {
+      const int t = (tid & 15) * 4, c = (u * 16 + (tid >> 4)) * 8;
+      if (u * 128 >= dh) break;
+      // words of new codes; single ones at [t0, t1)'s ends; words with old codes to move if the scale
+      // grew: what else is in them stays
+      if (c >= dh || t >= t1 || (t + 4 <= t0 && !grow)) continue;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t* to = (uint32_t*)(codes + (c + j) * PAGE + t);
+        uint32_t w = codes4(v[u][0][j], v[u][1][j], v[u][2][j], v[u][3][j], inv);
+        if (!grow && (t < t0 || t + 4 > t1)) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (t + k >= t0 && t + k < t1) ((uint8_t*)to)[k] = (uint8_t)(w >> (8 * k));
+          continue;
+        }
+        if (t < t0 || t + 4 > t1) {
+          const uint32_t was = *to, kept = grow ? recode4(was, move) : was, fresh = w;
+          w = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            w |= (t + k < t0 ? kept : t + k < t1 ? fresh : was) & (0xFFu << (8 * k));
+        }
+        *to = w;
+      }
+    }
   }
+  if (tid == 0 && (t0 == 0 || e > old)) *scale = (uint8_t)e;
 }
 
 // --------------------------------------------------------------------------------- attention
@@ -970,7 +1069,7 @@ extern "C" int32_t nv_op_kv8_append(const void* k, int64_t ldk, int64_t k_row_st
   if (rows == 0 || T == 0 || n_pages == 0 || table_w == 0) return NV_OK;
   NV_CHECK_ARG(k && v && kp && vp && ks && vs && table && pos, "null pointer argument");
   NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
-  const Kv8AppendArgs a{(const uint8_t*)k, (const uint8_t*)v, (uint8_t*)kp, (uint8_t*)vp, ks, vs,
+  const Kv8AppendArgs a{k, v, (uint8_t*)kp, (uint8_t*)vp, ks, vs,
                         ldk, k_row_stride, ldv, v_row_stride, n_pages, table, pos, count,
                         T, heads, dh, table_w};
   const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
@@ -979,8 +1078,18 @@ extern "C" int32_t nv_op_kv8_append(const void* k, int64_t ldk, int64_t k_row_st
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
   };
-  if (dtype == NV_F16) vec ? go(kv8_append_k<_Float16, true>) : go(kv8_append_k<_Float16, false>);
-  else vec ? go(kv8_append_k<__bf16, true>) : go(kv8_append_k<__bf16, false>);
+  const int64_t units = touched * heads * 2 * rows;  // below 2^33
+  auto few = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(units, 4)), dim3(256), 0, (hipStream_t)stream,
+                       a, units, (int)touched);
+  };
+  if (T <= KV8_FEW_TOKENS && units <= (1 << 25)) {
+    if (dtype == NV_F16) vec ? few(kv8_append_few_k<_Float16, true>) : few(kv8_append_few_k<_Float16, false>);
+    else vec ? few(kv8_append_few_k<__bf16, true>) : few(kv8_append_few_k<__bf16, false>);
+  } else {
+    if (dtype == NV_F16) vec ? go(kv8_append_k<_Float16, true>) : go(kv8_append_k<_Float16, false>);
+    else vec ? go(kv8_append_k<__bf16, true>) : go(kv8_append_k<__bf16, false>);
+  }
   NV_LAUNCH_CHECK("kv8_append_k");
   return NV_OK;
 }

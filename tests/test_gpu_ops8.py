@@ -329,9 +329,10 @@ def test_append(T, dh, dtype):
     check_append(k, v, pages, table, pos, [T, 0, T // 2 + 1, T + 5, -3], H)
 
 
-def test_append_scales_grow_and_stay():
+@pytest.mark.parametrize("T", [2, 5, 40])
+def test_append_scales_grow_and_stay(T):
     """Old scales above, at and below what the new tokens need, old codes that become subnormal."""
-    R, H, dh, T = 4, 2, 64, 2
+    R, H, dh = 4, 2, 64
     for old in (90, 115, 118, 119, 120, 140, 254):
         pages = pages_np(old, R * 2, H, dh, old, old + 1)
         table = np.arange(R * 2, dtype=np.int32).reshape(R, 2)
