@@ -109,6 +109,9 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   constexpr int FB = (FN + HALF - 1) / HALF;  // column fragments of the next tile read per row block
   static_assert((BM + BN) / 8 % NW == 0 && GA % NW == 0 && 128 % WN == 0, "tile");
   static_assert(FM == 2 || FM % 4 == 0, "row blocks");
+  // Two buffers of large tiles: see the step below.
+  constexpr bool EARLY = STAGES == 2 && BM == 256;
+  static_assert(!EARLY || WM / 16 % NW == 0, "sets of loads");
   extern __shared__ __align__(16) unsigned char smem[];
   const int tid = threadIdx.x % NT, lane = tid & 63, li = lane & 15, kc = lane >> 4;
   const int team = KT == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
@@ -149,12 +152,27 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   // Groups j0 .. j1 - 1 of tile kt into ring buffer `slot`.  Chunks wholly past K, and tiles past
   // the last one (issued all the same: every wave keeps its number of loads in flight), are out
   // of range: zeros.
-  auto issue = [&](int kt, int slot, int j0, int j1) {
-    uint8_t* dst = ring + slot * TILE;
+  auto load_group = [&](int kt, int slot, int j) {
     const uint32_t k0 = kt < kt1 && kt * 128 + cch < g.K ? (uint32_t)kt * 128 : OOB;
+    lds_dma16(j * NW < GA ? rx : rw, voff[j] + k0, ring + slot * TILE + (j * NW + wave) * 1024);
+  };
+  auto issue = [&](int kt, int slot, int j0, int j1) {
 #pragma unroll
-    for (int j = j0; j < j1; ++j)
-      lds_dma16(j * NW < GA ? rx : rw, voff[j] + k0, dst + (j * NW + wave) * 1024);
+    for (int j = j0; j < j1; ++j) load_group(kt, slot, j);
+  };
+  // EARLY: a tile's groups in two sets: its columns and the first half of every wave's rows (read
+  // in the second half of the step before), and the rest.
+  auto late = [](int j) { return j * NW < GA && (j * NW % (WM / 8)) * 2 >= WM / 8; };
+  auto issue_set = [&](int kt, int slot, bool rest, int part, int parts) {
+    constexpr int NR = GA / NW / 2, NF = PER - NR;  // groups of the sets
+    const int n = rest ? NR : NF, a = part * n / parts, b = (part + 1) * n / parts;
+    int i = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (late(j) == rest) {
+        if (i >= a && i < b) load_group(kt, slot, j);
+        ++i;
+      }
   };
   // scale bytes of tiles kb .. kb + S8_TILES - 1, those of a lane's FM rows side by side
   // (a team without tiles left: those of the last tile, for its zeros)
@@ -221,7 +239,10 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   };
 
 #pragma unroll
-  for (int s = 0; s < STAGES; ++s) issue(kt0 + s, s, 0, PER);
+  for (int s = 0; s < STAGES; ++s) {
+    if constexpr (EARLY) issue_set(kt0 + s, s, false, 0, 1), issue_set(kt0 + s, s, true, 0, 1);
+    else issue(kt0 + s, s, 0, PER);
+  }
   stage_scales(kt0);
   wait_loads<0>();  // the scales' bytes are the newest loads
   ring_barrier();
@@ -236,6 +257,14 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   const bool cut = KT == 1 && g.K % 16 && kt1 == KB;
   const int full = kt0 + steps - (cut ? 1 : 0);
   int slot = 0, kt = kt0;
+  // With EARLY a second barrier ends the step: the next tile's columns and first rows have then
+  // been read by every wave, and their place takes tile kt + 3's half a tile before the rest: every
+  // load has one and a half tiles of time instead of one (8192^3 418 -> 403 us,
+  // 8192 x 8192 x 2048 146 -> 143, 8192 x 10240 x 5120 367 -> 365).
+  if constexpr (EARLY) {
+    wait_loads<0>();
+    ring_barrier();
+  }
   auto step = [&](const intx8(&fb)[FN], intx8(&fn)[FN]) {
     const uint8_t* t = ring + slot * TILE;
     const int next = slot + 1 == STAGES ? 0 : slot + 1;
@@ -245,10 +274,17 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
       fa[HALF + i] = frag(t + arow + (HALF + i) * 2048);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) mul(i, j, sc, fb);
+      for (int j = 0; j < FN; ++j) {
+        mul(i, j, sc, fb);
+        if constexpr (EARLY) {
+          issue_set(kt + 2, slot, false, i * FN + j, HALF * FN);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    wait_loads<(STAGES - 2) * PER>();  // this wave's loads of tile kt + 1, its reads of kt
+    // this wave's loads of tile kt + 1 (what is read below, with EARLY), its reads of kt
+    wait_loads<EARLY ? PER : (STAGES - 2) * PER>();
     ring_barrier();
     const Scales sn = scales(kt + 1);
 #pragma unroll
@@ -258,9 +294,15 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
         mul(HALF + i, j, sc, fb);
         if (j < FB && i * FB + j < FN) fn[i * FB + j] = frag(tn + brow + (i * FB + j) * 2048);
         if (j == (FB < FN ? FB : FN - 1)) fa[i] = frag(tn + arow + i * 2048);
-        issue(kt + STAGES, slot, (i * FN + j) * PER / (HALF * FN), (i * FN + j + 1) * PER / (HALF * FN));
+        if constexpr (EARLY) issue_set(kt + 2, slot, true, i * FN + j, HALF * FN);
+        else issue(kt + STAGES, slot, (i * FN + j) * PER / (HALF * FN),
+                   (i * FN + j + 1) * PER / (HALF * FN));
         __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    if constexpr (EARLY) {
+      wait_loads<PER>();  // the rest of tile kt + 1; this wave's reads of it
+      ring_barrier();
     }
     sc = sn;
     slot = next;
