@@ -44,12 +44,13 @@ struct Kv8Plan {
 // 200000 tokens of 8 heads 84 us with 512 workgroups, 89 with 1024, 97 with 2048 (every share ends in
 // a merge and a partial result).
 inline Kv8Plan kv8_plan(int64_t rows, int S, int heads, int kv_heads, int table_w) {
+  // products of three sizes are taken in float64: they may pass 64 bits before they are refused
   const int64_t cols = (int64_t)S * (heads / kv_heads), rh = rows * kv_heads;
   Kv8Plan p{};
-  if (cols > 32) p.tall = rh * ((cols + 127) / 128) > 256 ? 2 : 1;
-  const int tile = p.tall ? 64 * p.tall : 16;
-  p.col_tiles = (int)((cols + tile - 1) / tile);
-  const int64_t want = 512 / (rh * p.col_tiles), can = table_w / (p.tall ? 4 : 8);
+  if (cols > 32) p.tall = (double)rh * ((cols + 127) / 128) > 256. ? 2 : 1;
+  const int64_t tile = p.tall ? 64 * p.tall : 16, tiles = (cols + tile - 1) / tile;
+  p.col_tiles = (int)std::min<int64_t>(tiles, 0x7FFFFFFF);
+  const int64_t want = (int64_t)(512. / ((double)rh * tiles)), can = table_w / (p.tall ? 4 : 8);
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, can), KV8_MAX_SPLITS));
   return p;
 }

@@ -1039,10 +1039,13 @@ bool head_dim_ok(int dh) {
   return dh == 16 || dh == 32 || dh == 40 || dh == 64 || dh == 80 || dh == 128 || dh == 160;
 }
 
-size_t part_bytes(const Kv8Plan& p, int64_t queries, int dh, size_t* ml_at) {
+// Partial results; with more than one share there are at most 512 tiles of queries.
+size_t part_bytes(const Kv8Plan& p, int64_t rows, int S, int heads, int dh, size_t* ml_at) {
+  if (p.splits == 1) return 0;
+  const int64_t queries = rows * S * heads;
   const size_t o = align_up((size_t)queries * p.splits * dh * 4, 256);
   if (ml_at) *ml_at = o;
-  return p.splits > 1 ? o + align_up((size_t)queries * p.splits * 8, 256) : 0;
+  return o + align_up((size_t)queries * p.splits * 8, 256);
 }
 
 }  // namespace
@@ -1099,7 +1102,7 @@ extern "C" size_t nv_op_attention_kv8_workspace(int32_t rows, int32_t S, int32_t
   if (rows < 1 || S < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || !head_dim_ok(dh) ||
       table_w < 0)
     return 0;
-  return part_bytes(kv8_plan(rows, S, heads, kv_heads, table_w), (int64_t)rows * S * heads, dh,
+  return part_bytes(kv8_plan(rows, S, heads, kv_heads, table_w), rows, S, heads, dh,
                     nullptr);
 }
 
@@ -1139,7 +1142,7 @@ extern "C" int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row
     return NV_ERR_UNSUPPORTED;
   }
   size_t ml_at = 0;
-  const size_t need = part_bytes(p, (int64_t)rows * S * heads, dh, &ml_at);
+  const size_t need = part_bytes(p, rows, S, heads, dh, &ml_at);
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) {
     set_error("workspace missing, misaligned or smaller than nv_op_attention_kv8_workspace()");
     return NV_ERR_WORKSPACE;

@@ -147,6 +147,17 @@ def test_attention_kv8_refusals():
     assert N.lib.nv_op_attention_kv8_workspace(1, 1, 4, 3, 64, 1000) == 0
 
 
+def test_attention_kv8_more_queries_than_64_bits_count():
+    # tiles of queries that are a multiple of 2^32, and products past 2^63: refused, nothing raised
+    N = _lib()
+    for rows, S, H, G in ((1, 1 << 30, 1 << 10, 1), (1 << 30, 1 << 30, 1 << 30, 1 << 30),
+                          (1, (1 << 31) - 1, 1, 1), (1 << 30, 1 << 20, 64, 1)):
+        assert N.lib.nv_op_attention_kv8_workspace(rows, S, H, G, 16, 64) == 0
+        st = N.lib.nv_op_attention_kv8(D, H * 16, 0, N.NV_F16, D, D, D, D, 4, D, 64, D, None, rows, S,
+                                       H, G, 16, 1.0, D, H * 16, 0, D, 1 << 20, None)
+        assert st == N.NV_ERR_UNSUPPORTED, (rows, S, H, G)
+
+
 def test_wrappers_take_device_tensors_only():
     import paper_2312_04429_amd as P
     x, s = torch.zeros(2, 128, dtype=torch.float16), torch.zeros(2, 1, dtype=torch.uint8)
