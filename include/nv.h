@@ -518,10 +518,10 @@ int32_t nv_op_attention(const void* q, const void* k, const void* vt, void* out,
  * outputs may not overlap unless said.
  *
  * nv_op_quant8: x [M] rows of K (x_dtype NV_F32, NV_F16 or NV_BF16, ldx apart)
- *   into 8-bit form.  1 <= K.
+ *   into 8-bit form.  1 <= K <= 2^31 - 256 (beyond: NV_ERR_UNSUPPORTED).
  * nv_op_dequant8: the values of an 8-bit matrix in out_dtype (NV_F32, NV_F16,
  *   NV_BF16): float32 and bfloat16 hold every value exactly (but for results
- *   below 2^-126), float16 rounds and overflows to infinity.
+ *   below 2^-126), float16 rounds and overflows to infinity.  K as above.
  * nv_op_rmsnorm8: s = x + residual (NULL: x) in float32,
  *   y = s * weight / sqrt(mean(s^2) + eps) in float32 from that sum, written in
  *   8-bit form with block_rows 1; h (NULL: not written) receives s rounded to
@@ -582,7 +582,10 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
  *   token gets zeros.  Codes and scales of tokens that no query sees may hold
  *   anything, NaN among it.  float32 scores, softmax and sums; the
- *   probabilities enter the second product in float16.  scale finite.
+ *   probabilities enter the second product in float16.  With more than 32
+ *   queries a kv head, values whose scale is less than 2^-80 of the largest in
+ *   an earlier page of the row may lose bits (less than 2^-113: count as
+ *   zeros).  scale finite.
  *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV8_PAGE 64

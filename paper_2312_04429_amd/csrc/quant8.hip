@@ -230,6 +230,9 @@ void norm_launch(const NormArgs& a, bool vec, hipStream_t s) {
   return norm_go<T, 16, 4>(a, vec, s);
 }
 
+// Columns of a row: what the kernels' 32-bit column numbers reach, the last block's past its end
+// included.
+constexpr int32_t K_MAX = 0x7FFFFF00;
 bool half_type(int32_t t) { return t == NV_F16 || t == NV_BF16; }
 
 }  // namespace
@@ -245,6 +248,10 @@ extern "C" int32_t nv_op_quant8(const void* x, int32_t x_dtype, int64_t ldx, int
   NV_CHECK_ARG(x_dtype == NV_F32 || half_type(x_dtype), "x_dtype must be NV_F32, NV_F16 or NV_BF16");
   NV_CHECK_ARG(block_rows == 1 || block_rows == 128, "block_rows must be 1 or 128");
   NV_CHECK_ARG(ldx >= K && ldq >= K, "row strides shorter than K");
+  if (K > K_MAX) {
+    set_error("rows of more than 2^31 - 256 columns");
+    return NV_ERR_UNSUPPORTED;
+  }
   if (M == 0) return NV_OK;
   NV_CHECK_ARG(x && q && scales, "null pointer argument");
   const bool vec = K % 8 == 0 && ldx % 8 == 0 && ldq % 8 == 0 && aligned16(x) &&
@@ -267,6 +274,10 @@ extern "C" int32_t nv_op_dequant8(const void* q, int64_t ldq, const uint8_t* sca
                "out_dtype must be NV_F32, NV_F16 or NV_BF16");
   NV_CHECK_ARG(block_rows == 1 || block_rows == 128, "block_rows must be 1 or 128");
   NV_CHECK_ARG(ldo >= K && ldq >= K, "row strides shorter than K");
+  if (K > K_MAX) {
+    set_error("rows of more than 2^31 - 256 columns");
+    return NV_ERR_UNSUPPORTED;
+  }
   if (M == 0) return NV_OK;
   NV_CHECK_ARG(q && scales && out, "null pointer argument");
   const bool vec = K % 8 == 0 && ldo % 8 == 0 && ldq % 8 == 0 && aligned16(out) &&

@@ -74,6 +74,16 @@ def test_quant8_refusals():
     assert back(M=0) == N.NV_OK
 
 
+def test_quant8_rows_past_32_bit_columns():
+    N = _lib()
+    K = (1 << 31) - 1
+    for br in (1, 128):
+        assert N.lib.nv_op_quant8(D, N.NV_F16, K, 1, K, br, D, K, D, None) == N.NV_ERR_UNSUPPORTED
+        assert N.lib.nv_op_dequant8(D, K, D, 1, K, br, D, N.NV_F16, K, None) == N.NV_ERR_UNSUPPORTED
+    ok = (1 << 31) - 256
+    assert N.lib.nv_op_quant8(D, N.NV_F16, ok, 0, ok, 1, D, ok, D, None) == N.NV_OK
+
+
 def test_rmsnorm8_refusals():
     N = _lib()
 
