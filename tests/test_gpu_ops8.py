@@ -263,6 +263,18 @@ def test_linear8_strides():
     assert (big[:, :3] == 7).all() and (big[:, 3 + N:] == 7).all()
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 200, 300), (90, 333, 640), (700, 640, 256), (4100, 4200, 300)])
+def test_linear8_residual_is_the_output(M, N, K):
+    """The sum into the residual's own memory: the bits of the call that writes elsewhere."""
+    q, s = nv().nv_op_quant8(rand(0, M, K))
+    w, ws = nv().nv_op_quant8(rand(1, N, K), block_rows=128)
+    r = rand(2, M, N, dtype=BF16)
+    want = nv().nv_op_linear8(q, s, w, ws, residual=r, dtype=BF16)
+    got = r.clone()
+    assert nv().nv_op_linear8(q, s, w, ws, residual=got, dtype=BF16, out=got) is got
+    assert torch.equal(got, want) and not torch.isnan(got).any()
+
+
 def test_linear8_nan_stays_in_its_row_and_column():
     xq, xs = O.quantise(np.random.default_rng(0).standard_normal((70, 300)))
     wq, ws = O.quantise(np.random.default_rng(1).standard_normal((150, 300)), 128)
@@ -496,6 +508,23 @@ def test_attention_value_scales_far_apart():
             if dtype == F16:
                 pages[1][table[0]] &= 0x87  # small codes
             check_attention(q, pages, table, [320], 0.125, 1)
+
+
+@pytest.mark.parametrize("S", [40, 150])
+def test_attention_value_scales_far_apart_many_queries(S):
+    """The same where queries share pages (64 and 128 of them): exponents up to 80 apart, no limit
+    and a causal one."""
+    for order in ((100, 127, 145, 110, 127), (145, 100, 127, 70, 140), (40, 60, 90, 119, 120)):
+        pages, table = a_cache(2, 1, 5, 1, 64)
+        pages[3][table[0]] = np.array(order, np.uint8)[:, None]
+        pages[2][:] = 118
+        q = rand(3, 1, S, 64, dtype=BF16)
+        check_attention(q, pages, table, [320], 0.125, 1)
+        check_attention(q, pages, table, [310], 0.125, 1, [310 - S])
+    pages, table = a_cache(2, 130, 2, 1, 64)  # 130 rows: tiles of 128 queries
+    pages[3][table] = np.array([[145], [90]], np.uint8)
+    pages[2][:] = 118
+    check_attention(rand(3, 130, S, 64, dtype=BF16), pages, table, [120] * 130, 0.125, 1)
 
 
 def test_attention_peaked_and_large_scores():
