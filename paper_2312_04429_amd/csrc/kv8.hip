@@ -66,9 +66,8 @@ struct Appended {
 };
 
 // Up to KV8_FEW_TOKENS tokens a row: a wave for what a workgroup does below.  Its lanes take eight
-// channels of a token each; nothing waits for a barrier, and 32 registers keep the chip full of
-// them (200 rows of one token, 8 heads of 128: 16.7 us with the
-// kernel below, 7.1 here; four rows of 1000 tokens are the other kernel's, 13 us).
+// channels of a token each, and nothing waits for a barrier (200 rows of one token, 8 heads of 128:
+// 16.7 us with the kernel below, 7.1 here).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv8_append_few_k(Kv8AppendArgs a, int64_t units, int slots) {
   constexpr int MAXU = (KV8_FEW_TOKENS * 160 / 8 + 63) / 64;
@@ -1039,7 +1038,7 @@ bool head_dim_ok(int dh) {
   return dh == 16 || dh == 32 || dh == 40 || dh == 64 || dh == 80 || dh == 128 || dh == 160;
 }
 
-// Partial results; with more than one share there are at most 512 tiles of queries.
+// Partial results.
 size_t part_bytes(const Kv8Plan& p, int64_t rows, int S, int heads, int dh, size_t* ml_at) {
   if (p.splits == 1) return 0;
   const int64_t queries = rows * S * heads;
@@ -1102,7 +1101,7 @@ extern "C" size_t nv_op_attention_kv8_workspace(int32_t rows, int32_t S, int32_t
   if (rows < 1 || S < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || !head_dim_ok(dh) ||
       table_w < 0)
     return 0;
-  return part_bytes(kv8_plan(rows, S, heads, kv_heads, table_w), rows, S, heads, dh,
+  return part_bytes(kv8_plan(rows, S, heads, kv_heads, dh, table_w), rows, S, heads, dh,
                     nullptr);
 }
 
@@ -1135,7 +1134,7 @@ extern "C" int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row
     return NV_ERR_UNSUPPORTED;
   }
   NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
-  const Kv8Plan p = kv8_plan(rows, S, heads, kv_heads, table_w);
+  const Kv8Plan p = kv8_plan(rows, S, heads, kv_heads, dh, table_w);
   if ((int64_t)S * (heads / kv_heads) > 0x7FFFFFF0 ||
       (double)rows * kv_heads * p.col_tiles * p.splits > 8388607.0) {
     set_error("more queries than a grid holds");
