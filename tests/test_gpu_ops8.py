@@ -25,7 +25,7 @@ import pytest
 import torch
 
 from oracle import ops8 as O
-from ops8_sizes import FORM_SIZES
+from ops8_sizes import FORM_SIZES, PLAN_SIZES
 
 pytestmark = pytest.mark.gpu
 
@@ -485,6 +485,21 @@ def test_attention_tall():
                         [n - S for n in lens] if causal else None)
 
 
+@pytest.mark.parametrize("tile,shares", sorted(PLAN_SIZES))
+def test_attention_plans(tile, shares):
+    """Every tile of queries with every join of shares: rows of differing length, holes, a causal
+    limit."""
+    for i, (R, S, Hq, H, dh, W) in enumerate(PLAN_SIZES[tile, shares]):
+        print("attention_kv8 plan", R, S, Hq, H, dh, W, flush=True)
+        pages, table = a_cache(S + W, R, W, H, dh)
+        lens = [W * 64 - (W * 23 * r) % (W * 64) for r in range(R)]
+        spoil(pages, table, lens)
+        if i:
+            table[0, W // 2] = -1
+        q = rand(S + W, R, S, Hq * dh, dtype=(BF16, F16)[i])
+        check_attention(q, pages, table, lens, dh ** -0.5, H, [n - S for n in lens] if i else None)
+
+
 def test_attention_holes_and_bad_pages():
     R, H, dh, W = 3, 2, 64, 6
     pages, table = a_cache(1, R, W, H, dh)
@@ -521,10 +536,11 @@ def test_attention_value_scales_far_apart_many_queries(S):
         q = rand(3, 1, S, 64, dtype=BF16)
         check_attention(q, pages, table, [320], 0.125, 1)
         check_attention(q, pages, table, [310], 0.125, 1, [310 - S])
-    pages, table = a_cache(2, 130, 2, 1, 64)  # 130 rows: tiles of 128 queries
+    pages, table = a_cache(2, 320, 2, 1, 64)  # 320 rows: tiles of 128 queries for the larger S
     pages[3][table] = np.array([[145], [90]], np.uint8)
     pages[2][:] = 118
-    check_attention(rand(3, 130, S, 64, dtype=BF16), pages, table, [120] * 130, 0.125, 1)
+    check_attention(rand(3, 320, S - 50 if S > 64 else S, 64, dtype=BF16), pages, table, [120] * 320,
+                    0.125, 1)
 
 
 def test_attention_peaked_and_large_scores():

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from oracle import ops8 as O
-from ops8_sizes import FORM_SIZES
+from ops8_sizes import FORM_SIZES, PLAN_SIZES
 
 
 def test_oracle_codes_are_torchs_e4m3():
@@ -192,9 +192,15 @@ def rules(tmp_path_factory):
     src, out = str(d / "rule.cpp"), str(d / "rule.so")
     with open(src, "w") as f:
         f.write('''
+#include "kv8.h"
 #include "linear8.h"
 extern "C" int form(long long M, int N, int K) { return nv::linear8_form(M, N, K); }
 extern "C" int forms() { return nv::L8_COUNT; }
+extern "C" int few() { return nv::KV8_FEW; }
+extern "C" void plan(long long rows, int S, int heads, int kv_heads, int dh, int pages, int* out) {
+  const nv::Kv8Plan p = nv::kv8_plan(rows, S, heads, kv_heads, dh, pages);
+  out[0] = p.tall, out[1] = p.splits, out[2] = p.col_tiles;
+}
 ''')
     csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                         "paper_2312_04429_amd", "csrc")
@@ -210,6 +216,34 @@ def test_every_form_of_the_product_is_reached(rules):
     for form, sizes in FORM_SIZES.items():
         for s in sizes:
             assert rules.form(*s) == form, s
+
+
+def _plan(rules, rows, *sizes):
+    out = (C.c_int * 3)()
+    rules.plan(C.c_longlong(rows), *sizes, out)
+    return tuple(out)
+
+
+def test_every_tile_and_join_of_attention_is_reached(rules):
+    kind = lambda n: "one" if n == 1 else "few" if n <= rules.few() else "many"
+    for want, sizes in PLAN_SIZES.items():
+        for s in sizes:
+            tall, splits, tiles = _plan(rules, *s)
+            assert (tall, kind(splits)) == want, s
+            assert tiles == -(-s[1] * (s[2] // s[3]) // (16, 64, 128)[tall])
+
+
+def test_shares_of_attention_stay_in_bounds(rules):
+    """At most 256 shares (the join's threads), 1024 workgroups of shares, and a page a share."""
+    rng = np.random.default_rng(0)
+    for _ in range(4000):
+        rows, kv, group = (int(2 ** rng.uniform(0, t)) for t in (9, 6, 5))
+        S, W = int(2 ** rng.uniform(0, 15)), int(2 ** rng.uniform(0, 20))
+        dh = int(rng.choice([16, 32, 40, 64, 80, 128, 160]))
+        tall, splits, tiles = _plan(rules, rows, S, kv * group, kv, dh, W)
+        assert 1 <= splits <= 256 and (splits == 1 or splits <= W)
+        assert splits == 1 or splits * tiles * rows * kv <= 1024, (rows, S, kv, group, dh, W)
+        assert (tall > 0) == (S * group > 32) and tiles * (16, 64, 128)[tall] >= S * group
 
 
 # us of each form (0 .. 7 as in linear8.h; None: not taken or not timed), graph-timed on one MI355X
