@@ -12,6 +12,8 @@ from the paper's definitions:
                state served (Sec. 5.4);
   predictor.py the match predictor, a linear one-class SVM trained by SGD
                (Sec. 5.2, Sec. 6);
+  ops8.py      the 8-bit operators of a transformer layer: e4m3 form, norm, product,
+               paged key / value cache and its attention, in float64;
   ivf.py       an inverted-file approximate index over the cached embeddings
                (the indexed vector-DB search of Sec. 5.3 / Sec. 6).
 

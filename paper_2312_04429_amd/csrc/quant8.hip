@@ -2,7 +2,9 @@
 //
 // All three are bound by HBM: each value is read once into registers, its block's largest
 // magnitude is found there (a block of 128 columns is 16 lanes of 8 values: four DPP maxima,
-// no LDS), and codes leave as 8-byte stores, one scale byte per block.
+// no LDS), and codes leave as 8-byte stores, one scale byte per block.  Measured: 8192 x 5120
+// float16 into codes 26 us (4.8 TB/s read and written), back to bfloat16 22 (5.8); 10240 x 1280
+// float32 in blocks of 128 rows 13 (5.0); the norm of 16384 x 1280 with residual 31 (4.7).
 #include <algorithm>
 
 #include "common.h"
