@@ -25,7 +25,7 @@ struct Kv8AttnArgs {
   void* out;
   int64_t ldo, o_row;
   int col_tiles, splits, tall;  // as in Kv8Plan
-  float *part_o, *part_ml;    // per query and share: dh sums; (reference maximum, sum)
+  float *part_o, *part_ml;    // per query and share: dh means; (reference maximum, sum)
 };
 
 constexpr int KV8_MAX_SPLITS = 256, KV8_FEW = 8;  // shares at most; joined by a thread up to

@@ -479,7 +479,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
 
 // A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
 // share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
-// than one share the sums go to the workspace and attn_kv8_join_k adds them in order.  Bound by HBM:
+// than one share the means go to the workspace and attn_kv8_join_k adds them in order.  Bound by HBM:
 // one query over 200000 tokens, 8 heads of 128, 77 us (5.3 TB/s); 32 rows of 2048 to 8192 tokens 76.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
@@ -547,11 +547,12 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
     if (next >= 0) pc.load_values(a, next, li, kc);
     ph = next;
   }
-  // the waves' states, in wave order
-  const float l = rows_sum(st.l), us = scale_value(st.unit);
+  // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
+  // sum in its final size may pass float32 where the mean does not).
+  const float l = rows_sum(st.l), us = scale_value(st.unit), mean = l == 0.f ? 0.f : 1.f / l;
   if (kc == 0) sm[wave][li] = st.m, sl[wave][li] = l;
 #pragma unroll
-  for (int j = 0; j < D::DV; ++j) *(floatx4*)&so[wave][li][j * 16 + kc * 4] = st.acc[j] * us;
+  for (int j = 0; j < D::DV; ++j) *(floatx4*)&so[wave][li][j * 16 + kc * 4] = st.acc[j] * mean * us;
   __syncthreads();
   for (int i = tid; i < 16 * (CH / 4); i += 256) {
     const int c = i / (CH / 4), d = i % (CH / 4) * 4;
@@ -560,20 +561,18 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
 #pragma unroll
     for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][c]);
     const float base = m == -INFINITY ? 0.f : m;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    float ls = 0.f;
+    float f[NW], ls = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sm[w][c] - base);
-      ls += f * sl[w][c];
-      o += f * *(const floatx4*)&so[w][c][d];
-    }
+    for (int w = 0; w < NW; ++w) ls += f[w] = __builtin_amdgcn_exp2f(sm[w][c] - base) * sl[w][c];
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) o += f[w] * inv * *(const floatx4*)&so[w][c][d];
     if (a.splits == 1) {
       const int qi = (c0 + c) / group, h = head * group + (c0 + c) % group;
       struct alignas(8) Quad { T v[4]; } out;
-      const float inv = ls == 0.f ? 0.f : 1.f / ls;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)o[r];
       *(Quad*)((T*)a.out + (int64_t)row * a.o_row + (int64_t)qi * a.ldo + (int64_t)h * DH + d) = out;
     } else {
       const int64_t slot = (((int64_t)row * a.kv_heads + head) * cols + c0 + c) * a.splits + split;
@@ -907,7 +906,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
       for (int j = 0; j < D::DV; ++j) {
         const int d = j * 16 + kc * 4;
         if ((DH % 16 == 0 || d < DH) && (st[qb].m != -INFINITY || l != 0.f))
-          *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * us;
+          *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * inv * us;
       }
       if (kc == 0) a.part_ml[slot * 2] = st[qb].m, a.part_ml[slot * 2 + 1] = l;
       continue;
@@ -920,15 +919,15 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
       if (DH % 16 && d >= DH) continue;
       struct alignas(8) Quad { T v[4]; } out;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) out.v[r] = (T)(st[qb].acc[j][r] * us * inv);
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)(st[qb].acc[j][r] * inv * us);
       *(Quad*)(to + d) = out;
     }
   }
 }
 
-// The shares of a query's pages, in order.  A workgroup per query: the shares' factors first, then
-// GROUPS threads per four channels that take every GROUPS-th share and meet in LDS.  A share that
-// held nothing has no sums (its maximum is -inf, its sum 0).
+// The shares of a query's pages, in order.  A workgroup per query: the shares' weights first, then
+// GROUPS threads per four channels that take every GROUPS-th share's means and meet in LDS.  A share
+// that held nothing has no means (its maximum is -inf, its sum 0).
 template <typename T>
 __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
   __shared__ float fac[KV8_MAX_SPLITS];
@@ -946,27 +945,27 @@ __global__ void __launch_bounds__(256) attn_kv8_join_k(Kv8AttnArgs a) {
   __syncthreads();
   top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
   const float base = top == -INFINITY ? 0.f : top;
-  const float f = __builtin_amdgcn_exp2f(m - base);
-  if (tid < a.splits) fac[tid] = m == -INFINITY && l == 0.f ? -1.f : f;  // -1: no sums
-  const float ls = wave_sum(f * l);  // the same tree in every call
+  const float f = __builtin_amdgcn_exp2f(m - base) * l;
+  if (tid < a.splits) fac[tid] = m == -INFINITY && l == 0.f ? -1.f : f;  // -1: no means
+  const float ls = wave_sum(f);  // the same tree in every call
   if ((tid & 63) == 0) red[tid >> 6][1] = ls;
   __syncthreads();
   const float sum = (red[0][1] + red[1][1]) + (red[2][1] + red[3][1]);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int g = tid / nq, d = (tid - g * nq) * 4;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
   if (g < groups)
 #pragma unroll 4
     for (int s = g; s < a.splits; s += groups)
-      if (fac[s] != -1.f) o += fac[s] * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
+      if (fac[s] != -1.f) o += fac[s] * inv * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
   part[tid] = o;
   __syncthreads();
   if (tid >= nq) return;
   for (int i = 1; i < groups && i < a.splits; ++i) o += part[i * nq + tid];
   const int64_t row = rh / a.kv_heads, h = rh % a.kv_heads * group + c % group;
   struct alignas(8) Quad { T v[4]; } out;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+  for (int r = 0; r < 4; ++r) out.v[r] = (T)o[r];
   *(Quad*)((T*)a.out + row * a.o_row + c / group * a.ldo + h * a.dh + d) = out;
 }
 
@@ -980,29 +979,31 @@ __global__ void __launch_bounds__(256) attn_kv8_join_few_k(Kv8AttnArgs a) {
     const int64_t u = i / nq, rh = u / cols, c = u - rh * cols;
     const int d = (int)(i - u * nq) * 4;
     const float* ml = a.part_ml + u * a.splits * 2;
-    float m[KV8_FEW], l[KV8_FEW];
-    float top = -INFINITY;
+    float m[KV8_FEW], f[KV8_FEW];
+    float top = -INFINITY, ls = 0.f;
 #pragma unroll
     for (int s = 0; s < KV8_FEW; ++s) {
       m[s] = s < a.splits ? ml[s * 2] : -INFINITY;
-      l[s] = s < a.splits ? ml[s * 2 + 1] : 0.f;
+      f[s] = s < a.splits ? ml[s * 2 + 1] : 0.f;
       top = fmaxf(top, m[s]);
     }
     const float base = top == -INFINITY ? 0.f : top;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    float ls = 0.f;
+    bool none[KV8_FEW];
 #pragma unroll
     for (int s = 0; s < KV8_FEW; ++s) {
-      if (m[s] == -INFINITY && l[s] == 0.f) continue;
-      const float f = __builtin_amdgcn_exp2f(m[s] - base);
-      ls += f * l[s];
-      o += f * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
+      none[s] = m[s] == -INFINITY && f[s] == 0.f;
+      f[s] *= __builtin_amdgcn_exp2f(m[s] - base);
+      ls += f[s];
     }
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KV8_FEW; ++s)
+      if (!none[s]) o += f[s] * inv * *(const floatx4*)(a.part_o + (u * a.splits + s) * a.dh + d);
     const int64_t row = rh / a.kv_heads, h = rh % a.kv_heads * group + c % group;
     struct alignas(8) Quad { T v[4]; } out;
-    const float inv = ls == 0.f ? 0.f : 1.f / ls;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) out.v[r] = (T)(o[r] * inv);
+    for (int r = 0; r < 4; ++r) out.v[r] = (T)o[r];
     *(Quad*)((T*)a.out + row * a.o_row + c / group * a.ldo + h * a.dh + d) = out;
   }
 }

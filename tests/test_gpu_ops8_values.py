@@ -1,0 +1,57 @@
+"""Attention over the 8-bit cache where values, scores or sums are far from one another in size, against
+float64; the bound of each output is derived beside the helper that computes it."""
+import numpy as np
+import pytest
+import torch
+
+import ops8_values as V
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+# rows, queries: tiles of 16 with shares and without, of 64 and of 128
+PLANS = [(1, 3), (300, 3), (1, 40), (600, 40), (1, 150), (600, 150)]
+
+
+def nv():
+    import paper_2312_04429_amd as P
+    return P
+
+
+def run(q, pages, table, lens, scale, qpos=None, rows=1, dtype="bf16"):
+    """The call on `rows` rows that read the same pages: [S][Hq][dh] of the first; the others are equal
+    to the bit."""
+    _, S, Hq, dh = q.shape
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    rep = lambda a: dev(np.repeat(np.asarray(a, np.int32), rows, 0))
+    x = dev(q).to(TYPES[dtype]).reshape(1, S, Hq * dh).expand(rows, S, Hq * dh)
+    out = nv().nv_op_attention_kv8(x, tuple(dev(p) for p in pages), rep(table), rep(lens), scale,
+                                   qpos=None if qpos is None else rep(qpos))
+    assert (out.view(torch.int16) == out[:1].view(torch.int16)).all()
+    return out[0].double().cpu().numpy().reshape(S, Hq, dh)
+
+
+def check(q, pages, table, lens, scale, qpos=None, rows=1, dtype="bf16"):
+    print("attention_kv8", rows, q.shape, table.shape, lens, qpos, dtype, flush=True)
+    o, tol = V.attention(q, pages, table, lens, scale, qpos, dtype)
+    got = run(q, pages, table, lens, scale, qpos, rows, dtype)
+    with np.errstate(invalid="ignore"):
+        bad = ~(np.abs(got - o[0]) <= tol[0])
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(),
+                               float(np.nanmax(np.abs(got - o[0]) / tol[0])))
+    return o[0], got
+
+
+# ------------------------------------------------------------------------- values near the type's end
+
+@pytest.mark.parametrize("W", [5, 40, 320])
+@pytest.mark.parametrize("rows,S", PLANS)
+def test_sums_of_large_values(rows, S, W):
+    """Values of 2^120: their sum over the row passes float32, their mean does not."""
+    dh, rng = 64, np.random.default_rng(W)
+    kp = V.codes(rng, (W, 1, 64, dh), 0x20, 0x40)
+    vp = rng.integers(0x30, 0x39, (W, 1, dh, 64)).astype(np.uint8)
+    pages = [kp, vp, np.full((W, 1), 122, np.uint8), np.full((W, 1), 247, np.uint8)]
+    table = rng.permutation(W).reshape(1, W).astype(np.int32)
+    o, _ = check(V.queries(S, 1, dh), pages, table, [W * 64 - 7], 0.125, rows=rows)
+    assert o.min() > 2.0 ** 119
