@@ -305,7 +305,8 @@ __device__ __forceinline__ void share_of(int pages, int split, int splits, int* 
 }
 
 // One wave's running softmax over 16 queries: reference maximum, this lane's share of the sum,
-// accumulators O^T in units of 2^(unit - 127).
+// accumulators O^T in units of 2^(unit - 127).  The unit is a query's own: it follows the scales of the
+// pages that the query sees, and no others.
 template <int DH>
 struct State {
   float m, l;
@@ -352,8 +353,8 @@ struct PageCodes {
 };
 
 // A page's 64 tokens, from token j0 of the sequence, into the state.  lim: tokens this lane's
-// query sees; len: tokens of the sequence; some: whether some query sees only part of them.
-// keys_done runs once the keys' registers are free again.
+// query sees (at least one query sees some of the page); len: tokens of the sequence; some: whether
+// some query sees only part of them.  keys_done runs once the keys' registers are free again.
 template <typename T, int DH, typename Done>
 __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::Vec* fq,
                                           PageCodes<DH>& pc, float scale2, int j0, int lim, int len,
@@ -363,7 +364,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
   using V = Mma<_Float16>;
   u32x4(&v)[D::DV] = pc.v;
   const int ke = __builtin_amdgcn_readfirstlane(pc.ke);
-  int ve = __builtin_amdgcn_readfirstlane(pc.ve);
+  const int ve = __builtin_amdgcn_readfirstlane(pc.ve);
   floatx4 s[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
@@ -412,7 +413,6 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
   if (ve == 255) {  // a NaN scale: every code of the page is NaN, the unit stays
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) v[j] = u32x4{0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F};
-    ve = st.unit;
   }
   if (some) {
     // Tokens behind the sequence may hold anything: zeros.  A NaN among those before that some
@@ -450,24 +450,25 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
       }
     }
   }
-  int d = ve - st.unit;
-  if (d < UNIT_LO) {  // far below the unit: its own accumulators, added at their size
-    const float g = ldexpf(1.f, d);
+  // Queries that see the page have one unit (they saw the same pages before it), but for pages that
+  // come late (attn_kv8_tall_k).
+  const bool sees = lim > j0;
+  const int unit = __builtin_amdgcn_readlane(st.unit, __builtin_ctzll(__ballot(sees)));
+  const int d = ve == 255 ? 0 : ve - unit;
+  if (d < UNIT_LO || d > UNIT_HI || __ballot(sees && st.unit != unit)) {
+    // far from the unit: its own accumulators, added at their size; far above, it becomes the unit
+    const int own = ve == 255 ? 0 : ve - st.unit;
+    const bool up = sees && own > UNIT_HI;
+    const float was = up ? ldexpf(1.f, -own) : 1.f, g = up ? 1.f : sees ? ldexpf(1.f, own) : 0.f;
+    if (up) st.unit = ve;
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) {
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
       o = V::mul(V::codes(v[j][0], v[j][1], 1.f), fp[0], o);
       o = V::mul(V::codes(v[j][2], v[j][3], 1.f), fp[1], o);
-      st.acc[j] += o * g;
+      st.acc[j] = st.acc[j] * was + o * g;
     }
     return;
-  }
-  if (d > UNIT_HI) {  // far above: it becomes the unit
-    const float g = ldexpf(1.f, -d);
-#pragma unroll
-    for (int j = 0; j < D::DV; ++j) st.acc[j] *= g;
-    st.unit = ve;
-    d = 0;
   }
   const float g = __int_as_float((127 + d) << 23);
 #pragma unroll
@@ -639,7 +640,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
       const int d = D::dim(b, kc);
       fq[qb][b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
     }
-    st[qb].m = -INFINITY, sum[qb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    st[qb].m = -INFINITY, st[qb].unit = 1, sum[qb] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) st[qb].acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
@@ -708,8 +709,9 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
     for (int i = tid; i < 2 * (VR - DH) * VROW; i += NT)
       sv[i / ((VR - DH) * VROW)][DH * VROW + i % ((VR - DH) * VROW)] = (_Float16)0.f;
 
-  // Unit of the accumulators, the same in every wave.  A page's exponent beside it is folded into
-  // its converted values where that is exact; one far above becomes the unit; for one far below the
+  // Unit of the accumulators, the same in every wave, of the queries that see the page at hand.  A
+  // page's exponent beside it is folded into its converted values where that is exact; one far above
+  // becomes the unit (of the queries that see it: the others keep theirs); for one far below the
   // accumulators are brought to its size and back (exact too: they stay far from float32's ends; an
   // exponent more than 80 below leaves the rest to the conversion, and one more than 113 below
   // counts for nothing).
@@ -845,9 +847,13 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
     const bool some = j0 + PAGE > wave_least;  // some query of the wave sees part of it
     if (h.pre != 1.f) {
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb)
+      for (int qb = 0; qb < QB; ++qb) {
+        const bool sees = lim[qb] > j0;
+        const float f = sees || h.post != 1.f ? h.pre : 1.f;
+        if (sees && h.post == 1.f) st[qb].unit = p.ve;
 #pragma unroll
-        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= h.pre;
+        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= f;
+      }
     }
     if (j0 < wave_most && !(j0 + PAGE > least && (nan_pages >> (p.p - least / PAGE) & 1)))
       attend(p, buf, j0, some);
@@ -885,10 +891,9 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   }
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    st[qb].unit = unit;
     st[qb].l = kc == 0 ? sum[qb][0] : 0.f;
     for (int p = least / PAGE; p < pages; ++p) {
-      if (!(nan_pages >> (p - least / PAGE) & 1)) continue;
+      if (!(nan_pages >> (p - least / PAGE) & 1) || !__ballot(lim[qb] > p * PAGE)) continue;
       const int64_t ph = (int64_t)table[p] * a.kv_heads + head;  // there: its codes were read
       PageCodes<DH> pc;
       pc.load_keys(a, ph, li, kc);

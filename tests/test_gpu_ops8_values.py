@@ -55,3 +55,34 @@ def test_sums_of_large_values(rows, S, W):
     table = rng.permutation(W).reshape(1, W).astype(np.int32)
     o, _ = check(V.queries(S, 1, dh), pages, table, [W * 64 - 7], 0.125, rows=rows)
     assert o.min() > 2.0 ** 119
+
+
+# ---------------------------------------------------------------------- scales that a query does not see
+
+@pytest.mark.parametrize("order", ["last", "middle"])
+@pytest.mark.parametrize("rows,S", [(1, 5), (300, 5), (1, 60), (600, 60), (1, 120), (600, 120)])
+def test_scales_behind_the_limit_leave_a_query_alone(rows, S, order):
+    """Some queries of a tile see a page whose values are 2^150 times those before it, the others end
+    before it: theirs are the bits of a call without that page."""
+    pages, table = V.far_cache(150, order, top=250)
+    first = 64 * V.ORDERS[order].index(0)            # token where the large page begins
+    q, n = V.queries(S, 1, 64), 64 * table.shape[1]
+    qpos = [first - S // 2]                          # queries 0 .. S // 2 - 1 end before it
+    _, got = check(q, pages, table, [n], 0.125, qpos, rows)
+    o, alone = check(q, pages, table, [first], 0.125, qpos, rows)
+    assert np.array_equal(got[:S // 2], alone[:S // 2]) and (o[:S // 2] != 0).all()
+
+
+@pytest.mark.parametrize("rows,S", [(1, 60), (600, 60), (1, 120), (600, 120)])
+def test_nan_page_beside_scales_behind_the_limit(rows, S):
+    """The same with a NaN value in the last page that all queries see part of: it waits for the end."""
+    pages, table = V.far_cache(150, "last", top=250)
+    q = V.queries(S, 1, 64)
+    pages[1][table[0, 3], 0, 50, 63] = 0x7F          # token 255: seen by the second half
+    qpos = [256 - S // 2 - 1]
+    o, tol = V.attention(q, pages, table, [320], 0.125, qpos)
+    got = run(q, pages, table, [320], 0.125, qpos, rows)
+    assert np.array_equal(np.isnan(got), np.isnan(o[0])) and np.isnan(got).any()
+    with np.errstate(invalid="ignore"):
+        assert not (np.abs(got - o[0]) > tol[0]).any()
+    assert (got[:S // 2, 0, :50] != 0).all()
