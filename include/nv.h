@@ -582,10 +582,9 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
  *   token gets zeros.  Codes and scales of tokens that no query sees may hold
  *   anything, NaN among it.  float32 scores, softmax and sums; the
- *   probabilities enter the second product in float16.  With more than 32
- *   queries a kv head, values whose scale is less than 2^-80 of the largest in
- *   an earlier page of the row may lose bits (less than 2^-113: count as
- *   zeros).  scale finite.
+ *   probabilities enter the second product in float16.  Its sums are kept in
+ *   units of the largest value scale that the query sees: what is below 2^-126
+ *   of that loses bits.  scale finite.
  *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV8_PAGE 64

@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
 // page_step takes them, so 16 rows are 16 consecutive ones.  A page that not every query sees whole
 // has its scores masked and its values behind the sequence zeroed; one with a NaN value among the
 // others waits until the loop is over and goes through page_step, which keeps it from the queries
-// that do not see it.  Workgroups run in order of falling work under a causal limit: the last
+// that do not see it, and so does one whose values are too small beside the others'.  Workgroups run in order of falling work under a causal limit: the last
 // queries of every head first (short tiles beside long ones on a unit: equal within 2 %).
 // 2 x 2048 queries, 16 heads of 128 on 4, over 4096 tokens: 163 us (840 TFLOP/s), 152 under a
 // causal limit.  Per SIMD the matrix unit is busy 41 % of the time and the vector unit 44 %, mostly
@@ -650,6 +650,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   const int least = sees(c0);
   int pnext, pages;  // the next page of this share, and its end
   share_of((sees(c0 + COLS - 1) + PAGE - 1) / PAGE, split, a.splits, &pnext, &pages);
+  const int first = pnext;
   const int wave_least = sees(c0 + wave * QB * 16), wave_most = sees(c0 + (wave + 1) * QB * 16 - 1);
   // The next page that is there (p.ph < 0: none left).  Its table entry was read at the last call:
   // the page's address does not wait for memory.
@@ -712,22 +713,19 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   // Unit of the accumulators, the same in every wave, of the queries that see the page at hand.  A
   // page's exponent beside it is folded into its converted values where that is exact; one far above
   // becomes the unit (of the queries that see it: the others keep theirs); for one far below the
-  // accumulators are brought to its size and back (exact too: they stay far from float32's ends; an
-  // exponent more than 80 below leaves the rest to the conversion, and one more than 113 below
-  // counts for nothing).
+  // accumulators are brought to its size and back (exact too: they stay below 2^104), and one further
+  // below than that waits until the loop is over (sums of its own here cost every page 4 %).
+  constexpr int FAR = -80;
   int unit = 1;
-  struct How { float conv, pre, post; };  // factors of the values; of the accumulators, before, after
+  bool late = false;                               // some page waits for its distance
+  struct How { float conv, pre, post; bool late; };  // factors: values; accumulators before, after
   auto how = [&](const Page& p) {
     const int d = p.ve == 255 ? 0 : p.ve - unit;
-    How h{1.f, 1.f, 1.f};
-    if (d > UNIT_HI) {
-      h.pre = ldexpf(1.f, -d), unit = p.ve;
-    } else if (d < UNIT_LO) {
-      const int e = std::max(d, -80);
-      h.pre = ldexpf(1.f, -e), h.post = ldexpf(1.f, e), h.conv = ldexpf(1.f, std::max(d - e, -126));
-    } else {
-      h.conv = __int_as_float((127 + d) << 23);
-    }
+    How h{1.f, 1.f, 1.f, d < FAR};
+    if (d > UNIT_HI) h.pre = ldexpf(1.f, -d), unit = p.ve;
+    else if (h.late) late = true;
+    else if (d < UNIT_LO) h.pre = ldexpf(1.f, -d), h.post = ldexpf(1.f, d);
+    else h.conv = __int_as_float((127 + d) << 23);
     return h;
   };
 
@@ -855,7 +853,8 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
         for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= f;
       }
     }
-    if (j0 < wave_most && !(j0 + PAGE > least && (nan_pages >> (p.p - least / PAGE) & 1)))
+    if (j0 < wave_most && !h.late &&
+        !(j0 + PAGE > least && (nan_pages >> (p.p - least / PAGE) & 1)))
       attend(p, buf, j0, some);
     if (h.post != 1.f) {
 #pragma unroll
@@ -866,7 +865,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   };
 
   Page cur, ahead;
-  How hc{1.f, 1.f, 1.f};
+  How hc{1.f, 1.f, 1.f, false};
   if (tid == 0) nan_pages = 0;
   __syncthreads();
   take(cur);
@@ -892,8 +891,18 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     st[qb].l = kc == 0 ? sum[qb][0] : 0.f;
-    for (int p = least / PAGE; p < pages; ++p) {
-      if (!(nan_pages >> (p - least / PAGE) & 1) || !__ballot(lim[qb] > p * PAGE)) continue;
+    // the pages that wait: the units again in order tell which are too far below theirs
+    int seen_unit = 1;
+    for (int p = late ? first : least / PAGE; p < pages; ++p) {
+      bool waits = p >= least / PAGE && (nan_pages >> (p - least / PAGE) & 1);
+      if (late) {
+        const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
+        if (page < 0 || page >= a.n_pages) continue;
+        const int ve = __builtin_amdgcn_readfirstlane(a.vs[page * a.kv_heads + head]);
+        if (ve != 255 && ve > seen_unit + UNIT_HI) seen_unit = ve;
+        waits |= ve - seen_unit < FAR;
+      }
+      if (!waits || !__ballot(lim[qb] > p * PAGE)) continue;
       const int64_t ph = (int64_t)table[p] * a.kv_heads + head;  // there: its codes were read
       PageCodes<DH> pc;
       pc.load_keys(a, ph, li, kc);

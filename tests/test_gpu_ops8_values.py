@@ -86,3 +86,17 @@ def test_nan_page_beside_scales_behind_the_limit(rows, S):
     with np.errstate(invalid="ignore"):
         assert not (np.abs(got - o[0]) > tol[0]).any()
     assert (got[:S // 2, 0, :50] != 0).all()
+
+
+# --------------------------------------------------------------------------- value scales far apart
+
+@pytest.mark.parametrize("order", sorted(V.ORDERS))
+@pytest.mark.parametrize("rows,S", PLANS)
+def test_value_scales_far_apart(rows, S, order):
+    """Channels that only pages far below the largest scale decide, that page before and behind."""
+    for d in V.DISTANCES:
+        pages, table = V.far_cache(d, order)
+        q = V.queries(S, 1, 64)
+        n = 64 * table.shape[1]
+        check(q, pages, table, [n], 0.125, rows=rows)
+        check(q, pages, table, [n - 2], 0.125, [n - 2 - S], rows=rows)
