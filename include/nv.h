@@ -582,7 +582,9 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
  *   token gets zeros.  Codes and scales of tokens that no query sees may hold
  *   anything, NaN among it.  float32 scores, softmax and sums; the
- *   probabilities enter the second product in float16.  Its sums are kept in
+ *   probabilities enter the second product in float16, each rounded to 2^-11 of
+ *   itself or 2^-34 of the query's largest, and the same rounded ones make the
+ *   sum it is divided by.  The second product's sums are kept in
  *   units of the largest value scale that the query sees: what is below 2^-126
  *   of that loses bits.  scale finite.
  *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be

@@ -6,9 +6,12 @@
 // Attention multiplies 16-bit matrices: codes convert exactly (three mantissa bits), queries are
 // taken as they are, in their type, and scales stay out of the 16-bit operands: a page's key scale
 // multiplies its scores in float32, its value scale the accumulators' common unit.  The second
-// product is float16 for either type: probabilities of at most 256 lose 2^-11 there, 2^-8 in
-// bfloat16 (32 rows of up to 8192 tokens, bfloat16: error against float64 0.0022 -> 0.0017, of which
-// 0.0017 is the result's own rounding).
+// product is float16 for either type: a probability loses 2^-11 there, 2^-8 in bfloat16 (32 rows of up
+// to 8192 tokens, bfloat16: error against float64 0.0022 -> 0.0017, of which 0.0017 is the result's own
+// rounding).  Float16 has no small numbers, so the largest probability of a row stands at 2^15, or
+// 2^9 to 2^15 under many queries, instead of 1: one is rounded to 2^-11 of itself, or to 2^-34 of the
+// largest where it is subnormal (below 2^-23 of it).  The sum takes the same rounded ones: a tail that
+// rounding moves, moves the sum with it.
 // S^T = K Q^T is computed, so an accumulator entry's column is a query and the softmax state is a
 // lane's own; key row r of 16-key tile t is token 16 (r / 4) + 4 t + r % 4 of the page, so that
 // lane group kc ends up with tokens 16 kc .. 16 kc + 15: the probabilities are then the second
@@ -304,7 +307,7 @@ __device__ __forceinline__ void share_of(int pages, int split, int splits, int* 
   *p1 = std::min(*p0 + n, pages);
 }
 
-// One wave's running softmax over 16 queries: reference maximum, this lane's share of the sum,
+// One wave's running softmax over 16 queries: reference (probabilities are 2^(score - m)), their sum,
 // accumulators O^T in units of 2^(unit - 127).  The unit is a query's own: it follows the scales of the
 // pages that the query sees, and no others.
 template <int DH>
@@ -317,6 +320,17 @@ struct State {
 // The value exponents that convert exactly beside the unit: codes are 2^-9 .. 448, times
 // 2^-5 .. 2^7 still normal float16 numbers.
 constexpr int UNIT_LO = -5, UNIT_HI = 7;
+
+// The largest probability is at most 2^P_TOP, which float16 holds.
+constexpr float P_TOP = 15.f;
+
+// Sums over the 64 keys of a page out of the matrix unit, of the probabilities as rounded: a row of ones.
+__device__ __forceinline__ floatx4 add_probs(const half8* fp, floatx4 sum) {
+  half8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.f;
+  return Mma<_Float16>::mul(ones, fp[1], Mma<_Float16>::mul(ones, fp[0], sum));
+}
 
 // A lane's part of a page of one head: codes of keys 16 (li / 4) + 4 t + li % 4 and of 16 tokens of
 // channels 16 j + li, and the two scale bytes.
@@ -391,7 +405,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
       if (some && j0 + 16 * kc + 4 * t + r >= lim) s[t][r] = -INFINITY;
       top = fmaxf(top, s[t][r]);
     }
-  const float mnew = fmaxf(st.m, rows_max(top)), base = mnew == -INFINITY ? 0.f : mnew;
+  const float mnew = fmaxf(st.m, rows_max(top) - P_TOP), base = mnew == -INFINITY ? 0.f : mnew;
   const float alpha = __builtin_amdgcn_exp2f(st.m - base);
   if (__ballot(mnew != st.m)) {
 #pragma unroll
@@ -400,16 +414,12 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
     st.m = mnew;
   }
   half8 fp[2];
-  float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float p = __builtin_amdgcn_exp2f(s[t][r] - base);
-      sum += p;
-      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)p;
-    }
-  st.l += sum;
+    for (int r = 0; r < 4; ++r)
+      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[t][r] - base);
+  st.l += add_probs(fp, floatx4{0.f, 0.f, 0.f, 0.f})[0];
   if (ve == 255) {  // a NaN scale: every code of the page is NaN, the unit stays
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) v[j] = u32x4{0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F, 0x7F7F7F7F};
@@ -550,7 +560,7 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
   }
   // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
   // sum in its final size may pass float32 where the mean does not).
-  const float l = rows_sum(st.l), us = scale_value(st.unit), mean = l == 0.f ? 0.f : 1.f / l;
+  const float l = st.l, us = scale_value(st.unit), mean = l == 0.f ? 0.f : 1.f / l;
   if (kc == 0) sm[wave][li] = st.m, sl[wave][li] = l;
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) *(floatx4*)&so[wave][li][j * 16 + kc * 4] = st.acc[j] * mean * us;
@@ -713,9 +723,10 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   // Unit of the accumulators, the same in every wave, of the queries that see the page at hand.  A
   // page's exponent beside it is folded into its converted values where that is exact; one far above
   // becomes the unit (of the queries that see it: the others keep theirs); for one far below the
-  // accumulators are brought to its size and back (exact too: they stay below 2^104), and one further
-  // below than that waits until the loop is over (sums of its own here cost every page 4 %).
-  constexpr int FAR = -80;
+  // accumulators are brought to its size and back (exact too: a term is below 2^31, so they stay
+  // below 2^126), and one further below than that waits until the loop is over (sums of its own here
+  // cost every page 4 %).
+  constexpr int FAR = -64;
   int unit = 1;
   bool late = false;                               // some page waits for its distance
   struct How { float conv, pre, post; bool late; };  // factors: values; accumulators before, after
@@ -766,9 +777,11 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 #pragma unroll
     for (int j = 0; j < VG; ++j) fv[j][0] = value(j, 0), fv[j][1] = value(j, 1);
     __builtin_amdgcn_sched_barrier(0);
-    // scores relative to the query's reference; it moves only when one passes it by 2^8 (p stays
-    // below 256, as exact in 16 bits as below 1)
-    constexpr float MOVE = 8.f;
+    // Scores relative to the query's reference.  It moves only when a probability would pass 2^P_TOP,
+    // and then to where the largest is 2^LOW: low enough that few pages move it, high enough for what
+    // is small beside it (2 x 2048 queries of 16 heads on 4096 tokens, scores of spread 4: 161.8 us
+    // with 7, 165 with 9 and 10, 171 with 12; spread 1: 157 to 159 with any).
+    constexpr float LOW = 9.f;
     bool grow = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -792,7 +805,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
             top = fmaxf(top, s[qb][t][r]);
           }
       }
-      grow |= !(top <= MOVE) || st[qb].m == -INFINITY;
+      grow |= !(top <= P_TOP) || st[qb].m == -INFINITY;
     }
     if (__ballot(grow)) {
 #pragma unroll
@@ -804,8 +817,8 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
           for (int r = 0; r < 4; ++r) top = fmaxf(top, s[qb][t][r]);
         top = rows_max(top);
         const bool fresh = st[qb].m == -INFINITY;
-        const float move = fresh ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
-        const float mnew = fresh ? top : st[qb].m + move;
+        const float move = top == -INFINITY ? 0.f : fresh ? top - LOW : fmaxf(top - LOW, 0.f);
+        const float mnew = fresh ? top - LOW : st[qb].m + move;
         const float alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-move);
         st[qb].m = mnew;
         sum[qb] *= alpha;
@@ -815,10 +828,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
         for (int t = 0; t < 4; ++t) s[qb][t] -= move;
       }
     }
-    // the sums of the probabilities (as rounded) come out of the matrix unit, too: a row of ones
-    half8 fp[QB][2], ones;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.f;
+    half8 fp[QB][2];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
@@ -826,8 +836,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           fp[qb][t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[qb][t][r]);
-      sum[qb] = V::mul(ones, fp[qb][0], sum[qb]);
-      sum[qb] = V::mul(ones, fp[qb][1], sum[qb]);
+      sum[qb] = add_probs(fp[qb], sum[qb]);
     }
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) {
@@ -890,7 +899,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   }
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    st[qb].l = kc == 0 ? sum[qb][0] : 0.f;
+    st[qb].l = sum[qb][0];
     // the pages that wait: the units again in order tell which are too far below theirs
     int seen_unit = 1;
     for (int p = late ? first : least / PAGE; p < pages; ++p) {
@@ -911,7 +920,7 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
     }
     const float us = scale_value(st[qb].unit);
     const int col = c0 + (wave * QB + qb) * 16 + li;
-    const float l = rows_sum(st[qb].l);
+    const float l = st[qb].l;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (col >= cols) continue;
     if (a.splits > 1) {

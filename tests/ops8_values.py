@@ -5,8 +5,8 @@ E = 2^-23 a float32 operation, u(t) one rounding to t):
   scores         dh float32 additions and three products, the shift by the reference, the exponential:
                  dh E sum |q k| + 8 E |score| + 4 E of p, in numerator and denominator: twice of sum p |v|
   probabilities  rounded to float16, the same rounded ones above and below: u(float16) p each, twice, or
-                 where p is subnormal there 2^-25 of a reference that is 2^12 below the largest p or less:
-                 2^-37, of sum |v| above and of n |o| below
+                 where p is subnormal there 2^-25 of a reference that is 2^9 below the largest p or less:
+                 2^-34, of sum |v| above and of n |o| below
   sums           n terms in float32: n E of sum p |v|; sums that are kept in the unit of the largest
                  value scale that the query sees: 2^-149 of that scale for each of n terms
   result         u(t) |o|, and 2^-25 where a float16 result is subnormal (2^-134: bfloat16)
@@ -46,7 +46,7 @@ def attention(q, pages, table, lens, scale, qpos=None, dtype="bf16"):
     reach, top = seen_values(pages, table, lens, S, Hq, qpos)
     n = table.shape[1] * 64
     rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + 2 * U["f16"] + n * E
-    tol = rel * spread + 2.0 ** -37 * (reach + n * np.abs(o)) + n * 2.0 ** -149 * top
+    tol = rel * spread + 2.0 ** -34 * (reach + n * np.abs(o)) + n * 2.0 ** -149 * top
     tol = tol * (1 + U[dtype]) + U[dtype] * np.abs(o) + (2.0 ** -25 if dtype == "f16" else 2.0 ** -134)
     return o, tol
 
@@ -81,3 +81,25 @@ def far_cache(d, order, dh=64, top=200, seed=0):
 
 def queries(S, heads, dh, seed=1):
     return np.random.default_rng(seed).integers(-16, 17, (1, S, heads, dh)) / 16.0
+
+
+# One key 2^bits above all others in the sum, its value zero; scores of the others up to `spread` powers
+# of two apart.
+TAILS = [(20.0, 0.0), (25.1, 0.0), (24.5, 0.5), (24.5, 1.0), (28.0, 0.0)]
+
+
+def tail_cache(S, at, bits, spread, W=160, dh=64):
+    """(q, pages, table, tokens, scale) of one row and head with the large key at token `at`."""
+    rng = np.random.default_rng(3)
+    table = rng.permutation(W).reshape(1, W).astype(np.int32)
+    kp = np.zeros((W, 1, 64, dh), np.uint8)
+    q = np.zeros((1, S, 1, dh))
+    q[..., 0] = 1
+    if spread:
+        kp[:, 0, :, 1:] = codes(rng, (W, 64, dh - 1), 0x10, 0x20)
+        q[..., 1:] = rng.integers(-8, 9, (1, S, 1, dh - 1)) * (spread / 8)
+    vp = rng.integers(0x38, 0x48, (W, 1, dh, 64)).astype(np.uint8)     # 1 .. 4
+    kp[table[0, at // 64], 0, at % 64, 0] = 0x7E                       # 448
+    vp[table[0, at // 64], 0, :, at % 64] = 0
+    pages = [kp, vp, np.full((W, 1), 127, np.uint8), np.full((W, 1), 131, np.uint8)]
+    return q, pages, table, W * 64 - 5, bits * np.log(2) / 448

@@ -100,3 +100,16 @@ def test_value_scales_far_apart(rows, S, order):
         n = 64 * table.shape[1]
         check(q, pages, table, [n], 0.125, rows=rows)
         check(q, pages, table, [n - 2], 0.125, [n - 2 - S], rows=rows)
+
+
+# ------------------------------------------------------------------------------- small probabilities
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,S", PLANS)
+def test_tail_below_one_key(rows, S, dtype):
+    """One key far above all others, its value zero: the others' small probabilities are the result.
+    Flat tails, a tail that spreads, the key in the first page and behind."""
+    for at in (0, 3 * 64 + 9):
+        for bits, spread in V.TAILS:
+            q, pages, table, n, scale = V.tail_cache(S, at, bits, spread)
+            check(q, pages, table, [n], scale, rows=rows, dtype=dtype)
