@@ -572,6 +572,8 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   one, and then its old codes are rounded to that.  Codes of tokens behind the
  *   last one stay as they were; tokens past the table's end are dropped.  A page
  *   that is written may be named once among all rows.
+ *   rows <= 65535, heads <= 32767; T <= 2^30 - 128 or a table of fewer than 2^24 pages
+ *   a row (beyond: NV_ERR_UNSUPPORTED).
  *
  * nv_op_attention_kv8: o[i] = sum_j softmax_j(scale q[i] . k_j) v_j over the
  *   tokens j < lens[r] (device int32 [rows], clamped to the table's tokens) of

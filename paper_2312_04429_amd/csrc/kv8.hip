@@ -1104,6 +1104,10 @@ extern "C" int32_t nv_op_kv8_append(const void* k, int64_t ldk, int64_t k_row_st
                         T, heads, dh, table_w};
   const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
   const int64_t touched = std::min<int64_t>(((int64_t)T + PAGE - 2) / PAGE + 1, table_w);
+  if (touched > 0xFFFFFF) {  // 256 threads each: below 2^32 in all
+    set_error("tokens for more than 2^24 - 1 pages of a row");
+    return NV_ERR_UNSUPPORTED;
+  }
   const dim3 grid((unsigned)touched, heads * 2, rows);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
