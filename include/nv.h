@@ -521,9 +521,11 @@ int32_t nv_op_attention(const void* q, const void* k, const void* vt, void* out,
  *   into 8-bit form.  1 <= K <= 2^31 - 256 (beyond: NV_ERR_UNSUPPORTED).
  * nv_op_dequant8: the values of an 8-bit matrix in out_dtype (NV_F32, NV_F16,
  *   NV_BF16): float32 and bfloat16 hold every value exactly (but for results
- *   below 2^-126), float16 rounds and overflows to infinity.  K as above.
+ *   below 2^-126, and infinity from 2^128 on, which codes the library writes do
+ *   not reach), float16 rounds and overflows to infinity.  K as above.
  * nv_op_rmsnorm8: s = x + residual (NULL: x) in float32,
- *   y = s * weight / sqrt(mean(s^2) + eps) in float32 from that sum, written in
+ *   y = s * weight / sqrt(mean(s^2) + eps) in float32 from that sum (s^2 too: a
+ *   row of |s| above 2^60 or so overflows it and gives zeros), written in
  *   8-bit form with block_rows 1; h (NULL: not written) receives s rounded to
  *   dtype (NV_F16 or NV_BF16), the residual stream of the next layer; h may be
  *   x or residual itself with the same stride.  1 <= D <= 32768 (beyond:
@@ -545,10 +547,12 @@ int32_t nv_op_rmsnorm8(const void* x, int64_t ldx, const void* residual, int64_t
  *   NV_BF16).  Accumulation is float32, but for the matrix unit's own sums of
  *   eight consecutive k, which drop what is below 2^-13 of the largest of the
  *   eight products.  x and w 16-byte aligned, ldx and ldw multiples
- *   of 16 and >= K (NV_ERR_UNSUPPORTED otherwise); K any: the bytes of a row
- *   behind K may hold anything.  bias device f32 [N] or NULL; residual in
+ *   of 16, >= K and at most 4 MiB (NV_ERR_UNSUPPORTED otherwise); K any: every
+ *   row, the last included, is read up to the next multiple of 16 bytes, and
+ *   the bytes behind K may hold anything.  bias device f32 [N] or NULL; residual in
  *   dtype, ldr apart, or NULL; it may be out itself with the same stride.
- *   M <= 2^31 - 1.  No workspace. */
+ *   M <= 2^31 - 1; at most 2^23 - 1 output tiles (of 16 x 16 elements or more;
+ *   beyond: NV_ERR_UNSUPPORTED).  No workspace. */
 int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void* w, int64_t ldw,
                       const uint8_t* ws, const float* bias, const void* residual, int64_t ldr,
                       void* out, int64_t ldo, int32_t dtype, int64_t M, int32_t N, int32_t K,
@@ -571,9 +575,9 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   holds tokens before pos[r] keeps its scale unless a new token needs a larger
  *   one, and then its old codes are rounded to that.  Codes of tokens behind the
  *   last one stay as they were; tokens past the table's end are dropped.  A page
- *   that is written may be named once among all rows.
- *   rows <= 65535, heads <= 32767; T <= 2^30 - 128 or a table of fewer than 2^24 pages
- *   a row (beyond: NV_ERR_UNSUPPORTED).
+ *   that is written may be named once among all rows.  rows <= 65535, heads <=
+ *   32767; T <= 2^30 - 128 or fewer than 2^24 pages a row (beyond:
+ *   NV_ERR_UNSUPPORTED).
  *
  * nv_op_attention_kv8: o[i] = sum_j softmax_j(scale q[i] . k_j) v_j over the
  *   tokens j < lens[r] (device int32 [rows], clamped to the table's tokens) of
@@ -586,9 +590,9 @@ int32_t nv_op_linear8(const void* x, int64_t ldx, const uint8_t* xs, const void*
  *   anything, NaN among it.  float32 scores, softmax and sums; the
  *   probabilities enter the second product in float16, each rounded to 2^-11 of
  *   itself or 2^-34 of the query's largest, and the same rounded ones make the
- *   sum it is divided by.  The second product's sums are kept in
- *   units of the largest value scale that the query sees: what is below 2^-126
- *   of that loses bits.  scale finite.
+ *   sum it is divided by.  The second product's sums are kept in units of the
+ *   largest value scale that the query sees: what is below 2^-126 of that loses
+ *   bits.  scale finite.
  *   workspace: device, >= nv_op_attention_kv8_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV8_PAGE 64
