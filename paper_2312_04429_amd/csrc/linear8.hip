@@ -430,83 +430,56 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   }
 }
 
-// Few rows of x: bound by the bytes of w, which go straight from memory to registers.  A workgroup
-// takes NB * 16 columns and all of K; its eight waves take 128-deep tiles in turn (U at a time, all
-// their loads out before the first multiply) and their sums meet in LDS, in wave order.
-template <typename T, int MB, int NB, int U>
+// At most 16 rows of x: bound by the bytes of w, which go straight from memory to registers.  A
+// workgroup takes 16 columns and all of K; its eight waves take 128-deep tiles in turn (two at a time,
+// all their loads out before the first multiply) and their sums meet in LDS, in wave order.
+template <typename T>
 __global__ void __launch_bounds__(512) linear8_few_k(Linear8Args g) {
-  constexpr int NW = 8, ROW = NB * 16 + 4;
-  __shared__ __align__(16) float part[NW][MB * 16 * ROW];
+  constexpr int NW = 8, U = 2, ROW = 16 + 4;
+  __shared__ __align__(16) float part[NW][16 * ROW];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n0 = blockIdx.x * NB * 16;
+  const int n0 = blockIdx.x * 16;
   const int KB = (g.K + 127) / 128, k16 = (g.K + 15) & ~15;
-  const uint8_t *xr[MB], *xsr[MB], *wr[NB], *wsr[NB];
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int64_t m = std::min<int64_t>(i * 16 + li, g.M - 1);
-    xr[i] = g.x + m * g.ldx, xsr[i] = g.xs + m * KB;
-  }
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int64_t n = std::min(n0 + j * 16 + li, g.N - 1);
-    wr[j] = g.w + n * g.ldw;
-    wsr[j] = g.ws + (int64_t)(std::min(n0 + j * 16, g.N - 1) >> 7) * KB;
-  }
-  floatx4 acc[MB][NB];
-#pragma unroll
-  for (int i = 0; i < MB; ++i)
-#pragma unroll
-    for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  auto load = [&](const uint8_t* row, int kt) {  // chunks past the row's codes: its last one again
-    const u32x4 lo = *(const u32x4*)(row + std::min(kt * 128 + kc * 16, k16 - 16));
-    const u32x4 hi = *(const u32x4*)(row + std::min(kt * 128 + 64 + kc * 16, k16 - 16));
+  const int64_t row = std::min<int64_t>(li, g.M - 1), col = std::min(n0 + li, g.N - 1);
+  const uint8_t *xr = g.x + row * g.ldx, *xsr = g.xs + row * KB;
+  const uint8_t *wr = g.w + col * g.ldw, *wsr = g.ws + (int64_t)(n0 >> 7) * KB;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  auto load = [&](const uint8_t* codes, int kt) {  // chunks past the row's codes: its last one again
+    const u32x4 lo = *(const u32x4*)(codes + std::min(kt * 128 + kc * 16, k16 - 16));
+    const u32x4 hi = *(const u32x4*)(codes + std::min(kt * 128 + 64 + kc * 16, k16 - 16));
     return intx8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
                  (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
   for (int k0 = wave; k0 < KB; k0 += NW * U) {
-    intx8 fx[U][MB], fw[U][NB];
-    int sx[U][MB], sw[U][NB];
+    intx8 fx[U], fw[U];
+    int sx[U], sw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kt = std::min(k0 + u * NW, KB - 1);
-#pragma unroll
-      for (int j = 0; j < NB; ++j) fw[u][j] = load(wr[j], kt), sw[u][j] = wsr[j][kt];
-#pragma unroll
-      for (int i = 0; i < MB; ++i) fx[u][i] = load(xr[i], kt), sx[u][i] = xsr[i][kt];
+      fw[u] = load(wr, kt), sw[u] = wsr[kt];
+      fx[u] = load(xr, kt), sx[u] = xsr[kt];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int kt = k0 + u * NW;
       if (kt >= KB) break;  // uniform
       if ((kt + 1) * 128 > g.K) {
-#pragma unroll
-        for (int j = 0; j < NB; ++j) mask_tail(fw[u][j], g.K - kt * 128 - kc * 16);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) mask_tail(fx[u][i], g.K - kt * 128 - kc * 16);
+        mask_tail(fw[u], g.K - kt * 128 - kc * 16);
+        mask_tail(fx[u], g.K - kt * 128 - kc * 16);
       }
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              fw[u][j], fx[u][i], acc[i][j], 0, 0, 0, sw[u][j], 0, sx[u][i]);
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[u], fx[u], acc, 0, 0, 0, sw[u], 0,
+                                                             sx[u]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < MB; ++i)
-#pragma unroll
-    for (int j = 0; j < NB; ++j)
-      *(floatx4*)&part[wave][(i * 16 + li) * ROW + j * 16 + kc * 4] = acc[i][j];
+  *(floatx4*)&part[wave][li * ROW + kc * 4] = acc;
   __syncthreads();
-  for (int q = tid; q < MB * 16 * NB * 4; q += 512) {
-    const int m = q / (NB * 4), c = q % (NB * 4) * 4;
-    if (m >= g.M || n0 + c >= g.N) continue;
-    floatx4 v = *(const floatx4*)&part[0][m * ROW + c];
+  const int m = tid / 4, c = tid % 4 * 4;
+  if (tid >= 64 || m >= g.M || n0 + c >= g.N) return;
+  floatx4 v = *(const floatx4*)&part[0][m * ROW + c];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) v += *(const floatx4*)&part[w][m * ROW + c];
-    store_quad<T>(g, m, n0 + c, v);
-  }
+  for (int w = 1; w < NW; ++w) v += *(const floatx4*)&part[w][m * ROW + c];
+  store_quad<T>(g, m, n0 + c, v);
 }
 
 template <typename T, int BM, int BN, int WGM, int WGN, int KT, int STAGES>
@@ -526,8 +499,7 @@ template <typename T>
 hipError_t launch(const Linear8Args& g, int form, hipStream_t s) {
   switch (form) {
     case L8_FEW:
-      hipLaunchKernelGGL((linear8_few_k<T, 1, 1, 2>), dim3((unsigned)ceil_div(g.N, 16)), dim3(512),
-                         0, s, g);
+      hipLaunchKernelGGL(linear8_few_k<T>, dim3((unsigned)ceil_div(g.N, 16)), dim3(512), 0, s, g);
       return hipGetLastError();
     case 1: return go<T, 32, 32, 1, 1, 4, 4>(g, s);
     case 2: return go<T, 32, 64, 1, 2, 1, 4>(g, s);
