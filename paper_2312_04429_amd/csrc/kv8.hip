@@ -324,6 +324,13 @@ constexpr int UNIT_LO = -5, UNIT_HI = 7;
 // The largest probability is at most 2^P_TOP, which float16 holds.
 constexpr float P_TOP = 15.f;
 
+// The reference under which a score of `top` has the probability 2^room (room <= P_TOP): top - room, or
+// top itself where the scores are so large that this rounds to more than P_TOP below it.
+__device__ __forceinline__ float reference(float top, float room) {
+  const float low = top - room;
+  return top - low > P_TOP ? top : low;
+}
+
 // Sums over the 64 keys of a page out of the matrix unit, of the probabilities as rounded: a row of ones.
 __device__ __forceinline__ floatx4 add_probs(const half8* fp, floatx4 sum) {
   half8 ones;
@@ -405,7 +412,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
       if (some && j0 + 16 * kc + 4 * t + r >= lim) s[t][r] = -INFINITY;
       top = fmaxf(top, s[t][r]);
     }
-  const float mnew = fmaxf(st.m, rows_max(top) - P_TOP), base = mnew == -INFINITY ? 0.f : mnew;
+  const float mnew = fmaxf(st.m, reference(rows_max(top), P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
   const float alpha = __builtin_amdgcn_exp2f(st.m - base);
   if (__ballot(mnew != st.m)) {
 #pragma unroll
@@ -817,8 +824,9 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
           for (int r = 0; r < 4; ++r) top = fmaxf(top, s[qb][t][r]);
         top = rows_max(top);
         const bool fresh = st[qb].m == -INFINITY;
-        const float move = top == -INFINITY ? 0.f : fresh ? top - LOW : fmaxf(top - LOW, 0.f);
-        const float mnew = fresh ? top - LOW : st[qb].m + move;
+        const float low = reference(top, LOW);
+        const float move = low == -INFINITY ? 0.f : fresh ? low : fmaxf(low, 0.f);
+        const float mnew = fresh ? low : st[qb].m + move;
         const float alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-move);
         st[qb].m = mnew;
         sum[qb] *= alpha;

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import ops8_values as V
+from oracle import ops8 as O
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +114,28 @@ def test_tail_below_one_key(rows, S, dtype):
         for bits, spread in V.TAILS:
             q, pages, table, n, scale = V.tail_cache(S, at, bits, spread)
             check(q, pages, table, [n], scale, rows=rows, dtype=dtype)
+
+
+# ------------------------------------------------------------------------------------- large scores
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("rows,S", PLANS)
+def test_scores_of_any_size_pick_the_largest(rows, S, sign):
+    """Scores up to 2^40 whose neighbours lie far apart: the result is the value of one key, of either sign
+    of the scores, wherever that key is, and however the sum of a score and a small number rounds."""
+    dh, W = 64, 9
+    rng = np.random.default_rng(7)
+    table = rng.permutation(W).reshape(1, W).astype(np.int32)
+    vp = V.codes(rng, (W, 1, dh, 64), 0x20, 0x50)
+    q = np.zeros((1, S, 1, dh))
+    q[..., 0] = 1
+    for at in (5, 300, W * 64 - 1):
+        kp = np.zeros((W, 1, 64, dh), np.uint8)
+        kp[..., 0] = rng.integers(0x70, 0x7A, (W, 1, 64))          # 128 .. 320
+        kp[table[0, at // 64], 0, at % 64, 0] = 0x7E if sign > 0 else 0x68   # 448, 64
+        pages = [kp, vp, np.full((W, 1), 127, np.uint8), np.full((W, 1), 127, np.uint8)]
+        want = O.VALUES[vp[table[0, at // 64], 0, :, at % 64]]
+        for e in range(10, 41):
+            for m in (1.0, 1.13, 1.37, 1.71):
+                got = run(q, pages, table, [W * 64], sign * m * 2.0 ** e / 448, rows=rows, dtype="f16")
+                assert (got == want).all(), (at, e, m)
