@@ -59,10 +59,11 @@ inline double kv8_tall_cost(double rh, int64_t cols, int dh, int table_w, int ta
 // differing length even out (one query over 200000 tokens of 8 heads of 128: 1271 us in one piece, 78
 // in 32 shares, 84 in 128; 16 rows of 2048 to 8192: 38 with one, 41 with two a unit; 24 rows of
 // as many, 8 heads of 64: 41 and 32; 16 rows of 1000: 12.2 in one piece, 13.2 in two).  Beyond
-// that, of the tiles whose queries share a page (8 x 16 queries of 4 heads each, 4096 tokens: 34 us, tiles of 16
-// 48; 24 queries of 100000 tokens 66, tiles of 16 49), the cheaper by the cost above: of 105 sizes
-// (77 to 20000 tokens, dh 40 to 160) it takes 1.7 % more than the best measured choice on average, 16 %
-// at most (of 30 with up to 32 queries 2.8 %, 16 % at most).  Shares stay within 1024 workgroups, and so do the partial results (84 MB).
+// that, of the tiles whose queries share a page (8 x 16 queries of 4 heads each, 4096 tokens: 34 us,
+// tiles of 16 48; 24 queries of 100000 tokens 66, tiles of 16 49), the cheaper by the cost above: of
+// 105 sizes (77 to 20000 tokens, dh 40 to 160) it takes 1.7 % more than the best measured choice on
+// average, 16 % at most (of 30 with up to 32 queries 2.8 %, 16 % at most).  Shares stay within 1024
+// workgroups, and so do the partial results (84 MB).
 inline Kv8Plan kv8_plan(int64_t rows, int S, int heads, int kv_heads, int dh, int table_w) {
   // products of three sizes are taken in float64: they may pass 64 bits before they are refused
   const int64_t cols = (int64_t)S * (heads / kv_heads);

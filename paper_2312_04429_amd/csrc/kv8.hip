@@ -143,7 +143,7 @@ __device__ __forceinline__ float block_max(float v, float* part) {
 // for keys, and of four neighbouring tokens for values: their codes of one channel are a word of the
 // transposed page, sixteen lanes write a whole row of it, and nothing passes through LDS (through it,
 // byte by byte, 8 prompts of 2000 tokens, 8 heads of 128, took 28.8 us, so 23.6).  Bound by launch and
-// latency for single tokens, by HBM for prompts.
+// latency for single tokens; for prompts (3.8 TB/s) by its loads' way: waves wait 58 % of their cycles.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv8_append_k(Kv8AppendArgs a) {
   __shared__ float part[4];
@@ -498,7 +498,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Mma<T>::
 // A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
 // share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
 // than one share the means go to the workspace and attn_kv8_join_k adds them in order.  Bound by HBM:
-// one query over 200000 tokens, 8 heads of 128, 77 us (5.3 TB/s); 32 rows of 2048 to 8192 tokens 76.
+// one query over 200000 tokens, 8 heads of 128, 75 us (5.4 TB/s); 32 rows of 2048 to 8192 tokens 76.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
   using D = Dims<DH>;
@@ -606,11 +606,13 @@ __global__ void __launch_bounds__(256) attn_kv8_k(Kv8AttnArgs a) {
 // page_step takes them, so 16 rows are 16 consecutive ones.  A page that not every query sees whole
 // has its scores masked and its values behind the sequence zeroed; one with a NaN value among the
 // others waits until the loop is over and goes through page_step, which keeps it from the queries
-// that do not see it, and so does one whose values are too small beside the others'.  Workgroups run in order of falling work under a causal limit: the last
-// queries of every head first (short tiles beside long ones on a unit: equal within 2 %).
-// 2 x 2048 queries, 16 heads of 128 on 4, over 4096 tokens: 163 us (840 TFLOP/s), 152 under a
-// causal limit.  Per SIMD the matrix unit is busy 41 % of the time and the vector unit 44 %, mostly
-// one after the other.
+// that do not see it, and so does one whose values are too small beside the others'.  Workgroups run in
+// order of falling work under a causal limit: the last queries of every head first, which counts where
+// not all of them are resident at once.
+// 2 x 2048 queries, 16 heads of 128 on 4, over 4096 tokens: 154 us (890 TFLOP/s); per SIMD the matrix
+// unit is busy 41 % of the time and the vector unit 44 %, mostly one after the other.  Under a causal
+// limit behind 2048 tokens 133 to 138, from an empty cache 72: the 64 or 32 pages of the last tiles, at
+// 2.1 to 2.4 us a page, while the shorter tiles beside them end early (all 512 are resident).
 template <typename T, int DH, int QB>
 __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
   using D = Dims<DH>;

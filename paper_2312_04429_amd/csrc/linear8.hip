@@ -100,11 +100,11 @@ __device__ __forceinline__ void store_quad(const Linear8Args& g, int64_t m, int 
 // that runs out multiplies zeros (loads out of range), so all keep step with the barriers, and
 // the epilogue adds the teams' sums in order.
 //
-// Measured: 8192^3 403 us (2728 TFLOP/s), 8192 x 10240 x 5120 with bias 337 (2540): the multiplies take
-// 59 % of its cycles, and each round of 256 tiles adds about 14 us outside its steps, 6 of them the
-// results' stores.  2000 x 1280 x 5120 22 us: 160 tiles of 128 x 128 on 256 compute units, each bound by
-// the 96 KB of LDS that its waves read a step (two teams of 64 x 64 waves read 64 but hold two buffers
-// each, and took 28).
+// Measured: 8192 x 10240 x 5120 with bias 333 us in calls back to back (2580 TFLOP/s; graph replays of
+// a few calls, at a lower clock: 365, and 403 for 8192^3): the multiplies take 59 % of its cycles, and
+// each round of 256 tiles adds about 14 us outside its steps, 6 of them the results' stores.
+// 2000 x 1280 x 5120 22 us: 160 tiles of 128 x 128 on 256 compute units, each bound by the 96 KB of LDS
+// that its waves read a step (two teams of 64 x 64 waves read 64 but hold two buffers each, and took 28).
 template <typename T, int BM, int BN, int WGM, int WGN, int KT, int STAGES>
 __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) {
   constexpr int NW = WGM * WGN, NT = NW * 64;  // waves and threads of a team
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(KT * WGM * WGN * 64) linear8_k(Linear8Args g) 
   int slot = 0, kt = kt0;
   // With EARLY a second barrier ends the step: the next tile's columns and first rows have then
   // been read by every wave, and their place takes tile kt + 3's half a tile before the rest: every
-  // load has one and a half tiles of time instead of one (8192^3 418 -> 403 us,
+  // load has one and a half tiles of time instead of one (graph replays: 8192^3 418 -> 403 us,
   // 8192 x 8192 x 2048 146 -> 143, 8192 x 10240 x 5120 367 -> 365).
   if constexpr (EARLY) {
     wait_loads<0>();
