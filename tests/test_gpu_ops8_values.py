@@ -139,3 +139,21 @@ def test_scores_of_any_size_pick_the_largest(rows, S, sign):
             for m in (1.0, 1.13, 1.37, 1.71):
                 got = run(q, pages, table, [W * 64], sign * m * 2.0 ** e / 448, rows=rows, dtype="f16")
                 assert (got == want).all(), (at, e, m)
+
+
+@pytest.mark.parametrize("d", [20, 64, 65, 100, 120])
+@pytest.mark.parametrize("rows,S", [(1, 5), (300, 5), (1, 60), (600, 60), (1, 120), (600, 120)])
+def test_nan_page_beside_pages_far_below(rows, S, d):
+    """Both kinds of pages that may wait for the end of the loop, in one row and in one page, with a hole
+    between them."""
+    for at in (2, 4):
+        pages, table = V.far_cache(d, "first")
+        table[0, 3 if at == 4 else 1] = -1
+        pages[1][table[0, at], 0, 50, 63] = 0xFF
+        end = 64 * at + 64                           # the NaN's token is end - 1: the later half sees it
+        q, qpos = V.queries(S, 1, 64), [end - S // 2 - 1]
+        o, tol = V.attention(q, pages, table, [end], 0.125, qpos)
+        got = run(q, pages, table, [end], 0.125, qpos, rows)
+        assert np.array_equal(np.isnan(got), np.isnan(o[0])) and np.isnan(got).any()
+        with np.errstate(invalid="ignore"):
+            assert not (np.abs(got - o[0]) > tol[0]).any()
