@@ -907,13 +907,14 @@ __global__ void __launch_bounds__(256, 2) attn_kv8_tall_k(Kv8AttnArgs a) {
       buf ^= 1;
     }
   }
+  const uint32_t nans = __builtin_amdgcn_readfirstlane(nan_pages);
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     st[qb].l = sum[qb][0];
     // the pages that wait: the units again in order tell which are too far below theirs
     int seen_unit = 1;
-    for (int p = late ? first : least / PAGE; p < pages; ++p) {
-      bool waits = p >= least / PAGE && (nan_pages >> (p - least / PAGE) & 1);
+    for (int p = late ? first : nans ? least / PAGE : pages; p < pages; ++p) {
+      bool waits = p >= least / PAGE && (nans >> (p - least / PAGE) & 1);
       if (late) {
         const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
         if (page < 0 || page >= a.n_pages) continue;
