@@ -612,6 +612,105 @@ int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row_stride, in
                             size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ *
+ * Queries and keys between their product and the cache, and keys and values
+ * kept in 4 bits.  Sizes of zero (rows, S, T) are legal and launch nothing;
+ * strides are in elements; inputs and outputs may not overlap unless said.
+ *
+ * nv_op_qk_rope: each head of q (q_heads of dh channels: channel c of head h of
+ *   token s of row r at r * row_stride + s * ld + h * dh + c) and of k (k_heads;
+ *   0: none, its pointers may be NULL) is normed and rotated, in float32 with one
+ *   rounding to dtype (NV_F16 or NV_BF16) at the end.
+ *   norm = 1: y = x * w / sqrt(mean(x^2) + eps) over the head's dh channels (x^2 in
+ *   float32: a head of |x| above 2^60 or so overflows it and gives zeros), w =
+ *   q_weight, k_weight (device f32 [dh], NULL: ones); eps >= 0 and finite.
+ *   norm = 0: y = x, no weights.
+ *   Rotation: the first axes[0] + .. + axes[n_axes - 1] channels (HOST int32, each
+ *   even, 0 <= n_axes <= 4; beyond: NV_ERR_UNSUPPORTED) belong to the axes in turn;
+ *   pair i of all of them is turned by pos * freqs[i] radians (freqs: device f64, one
+ *   per pair, the axes' pairs one after another; pos: device int32, axis a of token s
+ *   of row r at r * pos_row_stride + s * ldpos + a, any value):
+ *     (u, v) -> (u cos - v sin, v cos + u sin).
+ *   halves = 0: a pair is two neighbouring channels; halves = 1: channel j of the
+ *   first half of its axis and channel j of the second.  Angles are float64 until
+ *   they are in [0, 1) turns.  Channels behind the axes are y.
+ *   dh a multiple of 8, 8 <= dh <= 256 (NV_ERR_UNSUPPORTED otherwise); strides of
+ *   any size (multiples of 8 with 16-byte aligned buffers are fastest), an
+ *   output's ld >= heads * dh.  An output may be its input with the same strides.
+ *   At most 2^20 heads and 2^23 - 1 tokens (beyond: NV_ERR_UNSUPPORTED).
+ * ------------------------------------------------------------------------ */
+int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_stride, void* q_out, int64_t ldqo,
+                      int64_t qo_row_stride, int32_t q_heads, const float* q_weight, const void* k,
+                      int64_t ldk, int64_t k_row_stride, void* k_out, int64_t ldko,
+                      int64_t ko_row_stride, int32_t k_heads, const float* k_weight, int32_t dtype,
+                      int32_t rows, int32_t S, int32_t dh, const int32_t* pos, int64_t ldpos,
+                      int64_t pos_row_stride, int32_t n_axes, const int32_t* axes,
+                      const double* freqs, int32_t halves, int32_t norm, float eps, void* stream);
+
+/* The 4-bit cache.  A page holds NV_KV4_PAGE = 64 consecutive tokens of one
+ * sequence: kp and vp [n_pages][heads][64][dh / 2] bytes of two e2m1 codes (OCP FP4:
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6, bit 3 the sign; channel 2 i in the low half of byte
+ * i), ks and vs [n_pages][heads][64][ceil(dh / 32)] one scale byte e for 32 channels
+ * of a token (the last block may be shorter): a value is code * 2^(e - 127), and e =
+ * 255 makes its block NaN.  The scale the library writes is the smallest e >= 1 with
+ * amax <= 6 * 2^(e - 127); codes are rounded to nearest even; a block that
+ * holds a NaN or an infinity becomes NaN.  table (device int32 [rows][table_w]) names
+ * the page of tokens 64 j .. 64 j + 63 of each row; an entry outside [0, n_pages) is a
+ * hole: its tokens are not stored and not seen.  dh in {16, 32, 40, 64, 80, 128, 160};
+ * kp and vp 16-byte aligned; rows <= 65535 (append, read); heads <= 32767.
+ *
+ * nv_op_kv4_append: the first count[r] (device int32 [rows], clamped to [0, T];
+ *   NULL: all T) tokens of row r of k and v (in dtype NV_F16 or NV_BF16; token t of row
+ *   r, head h at r * row_stride + t * ld + h * dh) become tokens pos[r] .. (device
+ *   int32 [rows]; a negative one stores nothing) of its sequence.  Only their own bytes
+ *   change: tokens that are there may be written again, in any order; tokens past the
+ *   table's end are dropped.  One place in the cache may be named once in a call.
+ *   T * heads * 4 ceil(dh / 32) < 2^32 - 255 (beyond: NV_ERR_UNSUPPORTED).
+ *
+ * nv_op_kv4_read: tokens pos[r] .. pos[r] + count[r] - 1 of each row's sequence as
+ *   k and v in dtype (NV_F32, NV_F16, NV_BF16), laid out as for append, rows of T
+ *   tokens; what is not held (past count[r] or the table's end, in a hole, pos[r] < 0)
+ *   is written as zeros.  float32 and bfloat16 hold every value exactly (but for
+ *   infinity from 2^128 on: largest magnitudes above 3.5 * 2^126), float16 rounds and
+ *   overflows to infinity.  T * heads * dh / 8 < 2^32 - 255.
+ *
+ * nv_op_attention_kv4: o[i] = sum_j softmax_j(scale q[i] . k_j) v_j over the
+ *   tokens j < lens[r] (device int32 [rows], clamped to the table's tokens) of
+ *   row r that are in no hole and, with qpos (device int32 [rows]; NULL: no
+ *   limit), j <= qpos[r] + i.  q and out in dtype (NV_F16, NV_BF16): query i of row r,
+ *   head h at r * row_stride + i * ld + h * dh (strides in multiples of 8, 16-byte
+ *   aligned: NV_ERR_UNSUPPORTED otherwise).  heads a multiple of kv_heads:
+ *   query head h reads kv head h / (heads / kv_heads).  A query that sees no
+ *   token gets zeros.  Codes and scales of tokens that no query sees may hold
+ *   anything, and a NaN block reaches only the queries that see its token: one of
+ *   keys their whole result, one of values its 32 channels.  float32 scores, softmax
+ *   and sums; the probabilities enter the second product rounded to 2^-11 of
+ *   themselves or 2^-34 of the query's largest, and the same rounded ones make the
+ *   sum it is divided by.  Values of 2^90 and more may overflow the sums, values below
+ *   2^-126 may count as zero.  scale finite.
+ *   workspace: device, >= nv_op_attention_kv4_workspace(...) bytes (0: may be
+ *   NULL), 256-byte aligned, contents need not be initialised. */
+#define NV_KV4_PAGE 64
+int32_t nv_op_kv4_append(const void* k, int64_t ldk, int64_t k_row_stride, const void* v,
+                         int64_t ldv, int64_t v_row_stride, int32_t dtype, int32_t rows,
+                         int32_t T, int32_t heads, int32_t dh, void* kp, void* vp, uint8_t* ks,
+                         uint8_t* vs, int64_t n_pages, const int32_t* table, int32_t table_w,
+                         const int32_t* pos, const int32_t* count, void* stream);
+int32_t nv_op_kv4_read(const void* kp, const void* vp, const uint8_t* ks, const uint8_t* vs,
+                       int64_t n_pages, const int32_t* table, int32_t table_w, const int32_t* pos,
+                       const int32_t* count, int32_t rows, int32_t T, int32_t heads, int32_t dh,
+                       void* k, int64_t ldk, int64_t k_row_stride, void* v, int64_t ldv,
+                       int64_t v_row_stride, int32_t dtype, void* stream);
+size_t nv_op_attention_kv4_workspace(int32_t rows, int32_t S, int32_t heads, int32_t kv_heads,
+                                     int32_t dh, int32_t table_w);
+int32_t nv_op_attention_kv4(const void* q, int64_t ldq, int64_t q_row_stride, int32_t dtype,
+                            const void* kp, const void* vp, const uint8_t* ks, const uint8_t* vs,
+                            int64_t n_pages, const int32_t* table, int32_t table_w,
+                            const int32_t* lens, const int32_t* qpos, int32_t rows, int32_t S,
+                            int32_t heads, int32_t kv_heads, int32_t dh, float scale, void* out,
+                            int64_t ldo, int64_t o_row_stride, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ *
  * Launch tracing for measurement.  While enabled, every kernel launch of the
  * families in family_mask carries a pair of HIP events that the dispatch
  * timestamps at the kernel's start and end (the first max_launches launches

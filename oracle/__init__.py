@@ -14,6 +14,8 @@ from the paper's definitions:
                (Sec. 5.2, Sec. 6);
   ops8.py      the 8-bit operators of a transformer layer: e4m3 form, norm, product,
                paged key / value cache and its attention, in float64;
+  ops4.py      the norm and rotation of queries and keys, the 4-bit form, its paged key / value
+               cache and attention over it, in float64;
   ivf.py       an inverted-file approximate index over the cached embeddings
                (the indexed vector-DB search of Sec. 5.3 / Sec. 6).
 

@@ -18,16 +18,22 @@ Entry points (same names as the C ABI in include/nv.h):
   nv_op_linear8     matrix product of 8-bit activations and weights
   nv_kv8_pages, nv_op_kv8_append, nv_op_attention_kv8  keys and values kept in 8 bits, and
                     attention over them
+  nv_rope_freqs, nv_op_qk_rope  queries and keys normed for each head and rotated by position, over
+                    one axis or several (time, height, width)
+  nv_kv4_pages, nv_op_kv4_append, nv_op_kv4_read, nv_op_attention_kv4  keys and values kept in 4 bits
+                    (e2m1, a power-of-two scale a block), read back, and attention over them
 
 Importing the package loads libnv.so and fails if it has not been built.
 """
 from .api import (NvIVF, NvLCBFU, NvUNet, nv_cache_insert, nv_cache_move_rows, nv_gather_pool,
                   nv_match_gate, nv_ocsvm_train, nv_table_update, nv_cache_lookup, nv_cache_lookup_gated, nv_cache_lookup_gated_workspace,
                   nv_cache_lookup_static, nv_cache_lookup_workspace, nv_gather_states,
-                  nv_kv8_pages, nv_op_attention, nv_op_attention_kv8,
-                  nv_op_attention_kv8_workspace, nv_op_conv3x3, nv_op_dequant8, nv_op_kv8_append,
-                  nv_op_linear, nv_op_linear8, nv_op_quant8,
-                  nv_op_rmsnorm8, nv_probe_peaks, nv_trace_disable,
+                  nv_kv4_pages, nv_kv8_pages, nv_op_attention, nv_op_attention_kv4,
+                  nv_op_attention_kv4_workspace, nv_op_attention_kv8,
+                  nv_op_attention_kv8_workspace, nv_op_conv3x3, nv_op_dequant8, nv_op_kv4_append,
+                  nv_op_kv4_read, nv_op_kv8_append,
+                  nv_op_linear, nv_op_linear8, nv_op_qk_rope, nv_op_quant8,
+                  nv_op_rmsnorm8, nv_rope_freqs, nv_probe_peaks, nv_trace_disable,
                   nv_trace_enable, nv_trace_read, nv_trace_records, nv_unet_param_count,
                   nv_unet_param_info, workspace)
 
@@ -37,8 +43,10 @@ from ._native import NV_FAM_LINEAR as FAM_LINEAR, NV_FAM_SCAN as FAM_SCAN
 __all__ = ["FAM_ATTN", "FAM_CONV", "FAM_LINEAR", "FAM_SCAN", "NvIVF", "NvLCBFU", "NvUNet",
            "nv_cache_move_rows", "nv_gather_pool", "nv_match_gate", "nv_ocsvm_train",
            "nv_table_update", "nv_cache_insert", "nv_cache_lookup", "nv_cache_lookup_gated", "nv_cache_lookup_gated_workspace", "nv_cache_lookup_static", "nv_cache_lookup_workspace", "nv_gather_states",
-           "nv_kv8_pages", "nv_op_attention", "nv_op_attention_kv8",
-           "nv_op_attention_kv8_workspace", "nv_op_conv3x3", "nv_op_dequant8", "nv_op_kv8_append",
-           "nv_op_linear", "nv_op_linear8", "nv_op_quant8",
-           "nv_op_rmsnorm8", "nv_probe_peaks", "nv_trace_disable", "nv_trace_enable",
+           "nv_kv4_pages", "nv_kv8_pages", "nv_op_attention", "nv_op_attention_kv4",
+           "nv_op_attention_kv4_workspace", "nv_op_attention_kv8",
+           "nv_op_attention_kv8_workspace", "nv_op_conv3x3", "nv_op_dequant8", "nv_op_kv4_append",
+           "nv_op_kv4_read", "nv_op_kv8_append",
+           "nv_op_linear", "nv_op_linear8", "nv_op_qk_rope", "nv_op_quant8",
+           "nv_op_rmsnorm8", "nv_rope_freqs", "nv_probe_peaks", "nv_trace_disable", "nv_trace_enable",
            "nv_trace_read", "nv_trace_records", "nv_unet_param_count", "nv_unet_param_info", "workspace"]

@@ -14,6 +14,7 @@ NV_OK, NV_ERR_INVALID_ARG, NV_ERR_UNSUPPORTED = 0, -1, -2
 NV_ERR_OUT_OF_MEMORY, NV_ERR_HIP, NV_ERR_WORKSPACE = -3, -4, -5
 NV_F32, NV_BF16, NV_F16 = 0, 1, 2
 NV_KV8_PAGE = 64
+NV_KV4_PAGE = 64
 NV_LOOKUP_STATIC_BYTES = 64 << 20
 NV_FAM_CONV, NV_FAM_LINEAR, NV_FAM_ATTN, NV_FAM_SCAN = 1, 2, 4, 8
 NV_UNET_GRAPHS = 1
@@ -104,6 +105,15 @@ _sigs = {
                                VP, I64, VP, I32, VP, VP, VP]),
     "nv_op_attention_kv8_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
     "nv_op_attention_kv8": (I32, [VP, I64, I64, I32, VP, VP, VP, VP, I64, VP, I32, VP, VP, I32,
+                                  I32, I32, I32, I32, F32, VP, I64, I64, VP, SZ, VP]),
+    "nv_op_qk_rope": (I32, [VP, I64, I64, VP, I64, I64, I32, VP, VP, I64, I64, VP, I64, I64, I32, VP,
+                            I32, I32, I32, I32, VP, I64, I64, I32, VP, VP, I32, I32, F32, VP]),
+    "nv_op_kv4_append": (I32, [VP, I64, I64, VP, I64, I64, I32, I32, I32, I32, I32, VP, VP, VP,
+                               VP, I64, VP, I32, VP, VP, VP]),
+    "nv_op_kv4_read": (I32, [VP, VP, VP, VP, I64, VP, I32, VP, VP, I32, I32, I32, I32, VP, I64, I64,
+                             VP, I64, I64, I32, VP]),
+    "nv_op_attention_kv4_workspace": (SZ, [I32, I32, I32, I32, I32, I32]),
+    "nv_op_attention_kv4": (I32, [VP, I64, I64, I32, VP, VP, VP, VP, I64, VP, I32, VP, VP, I32,
                                   I32, I32, I32, I32, F32, VP, I64, I64, VP, SZ, VP]),
 }
 for _name, (_res, _args) in _sigs.items():

@@ -764,9 +764,14 @@ def nv_op_attention_kv8(q, pages, table, lens, scale, qpos=None, out=None, ws=No
     cached tokens of each row; with qpos (int32 [rows]) query i of row r sees tokens up to
     qpos[r] + i.  Query heads share the cache's heads in equal groups.  ws: (owner, address,
     bytes) of nv_op_attention_kv8_workspace(...) bytes, or None: one for this call."""
+    return _attention(q, _pages(pages, _dev(q, "q")), table, lens, scale, qpos, out, ws,
+                      "nv_op_attention_kv8")
+
+
+def _attention(q, cache, table, lens, scale, qpos, out, ws, name):
     dev, (ldq, qr) = _dev(q, "q"), _strides3(q, "q")
     _want(q, "q", _HALF, dev)
-    kp, vp, ks, vs, n, H, dh = _pages(pages, dev)
+    kp, vp, ks, vs, n, H, dh = cache
     rows, S, cols = q.shape
     if cols == 0 or cols % (H * dh):
         raise ValueError(f"q needs a multiple of kv_heads * dh = {H * dh} columns")
@@ -785,12 +790,154 @@ def nv_op_attention_kv8(q, pages, table, lens, scale, qpos=None, out=None, ws=No
     if rows < 2:
         qr, orow = 0, 0
     if ws is None:
-        need = N.lib.nv_op_attention_kv8_workspace(rows, S, heads, H, dh, W)
+        need = getattr(N.lib, name + "_workspace")(rows, S, heads, H, dh, W)
         ws = workspace(need, q.device) + (need,) if need else (None, None, 0)
-    _call("nv_op_attention_kv8", dev, q.data_ptr(), ldq, qr, _DT[q.dtype], kp.data_ptr(),
+    _call(name, dev, q.data_ptr(), ldq, qr, _DT[q.dtype], kp.data_ptr(),
           vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, table.data_ptr(), W, lens.data_ptr(),
           _at(qpos), rows, S, heads, H, dh, scale, out.data_ptr(), ldo, orow, ws[1], ws[2])
     return out
+
+
+_F64 = (torch.float64,)
+_CODES4 = frozenset((torch.float4_e2m1fn_x2, torch.uint8))
+
+
+def nv_rope_freqs(axes, theta=10000.0, device="cuda"):
+    """The rotation's radians per position, one per channel pair of each axis in turn: theta ** (-2 i
+    / n) for pair i of an axis of n channels.  float64 [sum(axes) / 2], for nv_op_qk_rope."""
+    return torch.tensor([theta ** (-2.0 * i / n) for n in axes for i in range(n // 2)],
+                        dtype=torch.float64, device=device)
+
+
+def nv_op_qk_rope(q, k, dh, pos, axes, freqs, q_weight=None, k_weight=None, eps=1e-6, halves=False,
+                  out=None):
+    """(q', k'): every head of q [rows][S][heads * dh] and k [rows][S][kv_heads * dh] (float16,
+    bfloat16; k may be None) divided by its root mean square and weighted (weights float32 [dh];
+    eps=None: no norm), and its channel pairs rotated by position: axes gives the channels of each
+    axis in turn, pos [rows][S][len(axes)] int32 a token's place on each, freqs float64 the radians
+    per position of each pair (nv_rope_freqs).  halves: a pair is one channel of each half of its axis,
+    else two neighbours.  Channels behind the axes are not rotated.  out: (q', k') to write, which may
+    be (q, k)."""
+    dev, (ldq, qr) = _dev(q, "q"), _strides3(q, "q")
+    _want(q, "q", _HALF, dev)
+    rows, S, cols = q.shape
+    if dh < 1 or cols % dh or (k is not None and (k.dim() != 3 or k.shape[2] % dh)):
+        raise ValueError(f"q and k need a multiple of dh = {dh} columns")
+    if len(axes) and (pos.dim() != 3 or (len(axes) > 1 and pos.stride(2) != 1)):
+        raise ValueError("pos: [rows][S][axes] with contiguous axes expected")
+    _want(pos, "pos", _I32, dev, (rows, S, len(axes)))
+    _want(freqs, "freqs", _F64, dev, (sum(axes) // 2,), True)
+    ldk = kr = kh = 0
+    if k is not None:
+        _want(k, "k", (q.dtype,), dev, (rows, S, k.shape[2]))
+        (ldk, kr), kh = _strides3(k, "k"), k.shape[2] // dh
+    if eps is None and not (q_weight is None and k_weight is None):
+        raise ValueError("weights without a norm (eps is None)")
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _want(w, what, _F32, dev, (dh,), True)
+    if out is None:
+        out = (torch.empty((rows, S, cols), dtype=q.dtype, device=q.device),
+               None if k is None else torch.empty((rows, S, kh * dh), dtype=q.dtype, device=q.device))
+    qo, ko = out
+    _want(qo, "out[0]", (q.dtype,), dev, (rows, S, cols))
+    (ldqo, qor), ldko, kor = _strides3(qo, "out[0]"), 0, 0
+    if k is not None:
+        _want(ko, "out[1]", (q.dtype,), dev, (rows, S, kh * dh))
+        ldko, kor = _strides3(ko, "out[1]")
+    if S < 2:  # strides of dimensions of one are free; any that the kernel takes will do
+        ldq, ldk, ldqo, ldko = cols, kh * dh, cols, kh * dh
+    if rows < 2:
+        qr = kr = qor = kor = 0
+    _call("nv_op_qk_rope", dev, q.data_ptr(), ldq, qr, qo.data_ptr(), ldqo, qor, cols // dh,
+          _at(q_weight), _at(k), ldk, kr, _at(ko) if kh else None, ldko, kor, kh, _at(k_weight),
+          _DT[q.dtype], rows, S, dh, pos.data_ptr(), pos.stride(1), pos.stride(0), len(axes),
+          (C.c_int32 * len(axes))(*axes), freqs.data_ptr(), halves, eps is not None,
+          0.0 if eps is None else eps)
+    return qo, ko
+
+
+def nv_kv4_pages(n_pages, heads, dh, device):
+    """An empty 4-bit cache of n_pages pages of 64 tokens: (kp, vp [n_pages][heads][64][dh / 2] of two
+    codes a byte, ks, vs [n_pages][heads][64][ceil(dh / 32)]), all zeros."""
+    z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+    codes = lambda: z(n_pages, heads, N.NV_KV4_PAGE, dh // 2).view(torch.float4_e2m1fn_x2)
+    scales = lambda: z(n_pages, heads, N.NV_KV4_PAGE, -(-dh // 32)).view(torch.float8_e8m0fnu)
+    return codes(), codes(), scales(), scales()
+
+
+def _pages4(pages, dev):
+    """Checks a 4-bit cache and returns (kp, vp, ks, vs, n_pages, heads, dh)."""
+    kp, vp, ks, vs = pages
+    if kp.dim() != 4 or kp.shape[2] != N.NV_KV4_PAGE:
+        raise ValueError("kp must be [n_pages][heads][64][dh / 2]")
+    n, h, _, b = kp.shape
+    _want(kp, "kp", _CODES4, dev, None, True)
+    _want(vp, "vp", _CODES4, dev, kp.shape, True)
+    _want(ks, "ks", _SCALES, dev, (n, h, N.NV_KV4_PAGE, -(-b // 16)), True)
+    _want(vs, "vs", _SCALES, dev, ks.shape, True)
+    return kp, vp, ks, vs, n, h, 2 * b
+
+
+def nv_op_kv4_append(k, v, pages, table, pos, count=None):
+    """Write tokens to a 4-bit cache in place: the first count[r] (None: all) of row r of
+    k, v [rows][T][heads * dh] (float16, bfloat16) become tokens pos[r] .. of the sequence whose
+    pages table[r] names (int32 [rows][table_w]; pos, count int32 [rows])."""
+    dev, (ldk, kr), (ldv, vr) = _dev(k, "k"), _strides3(k, "k"), _strides3(v, "v")
+    _want(k, "k", _HALF, dev)
+    _want(v, "v", (k.dtype,), dev, k.shape)
+    kp, vp, ks, vs, n, H, dh = _pages4(pages, dev)
+    rows, T, cols = k.shape
+    if cols != H * dh:
+        raise ValueError(f"k and v need heads * dh = {H * dh} columns")
+    W = _table(table, rows, dev)
+    _want(pos, "pos", _I32, dev, (rows,), True)
+    if count is not None:
+        _want(count, "count", _I32, dev, (rows,), True)
+    _call("nv_op_kv4_append", dev, k.data_ptr(), ldk, kr, v.data_ptr(), ldv, vr, _DT[k.dtype], rows,
+          T, H, dh, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n, table.data_ptr(),
+          W, pos.data_ptr(), _at(count))
+
+
+def nv_op_kv4_read(pages, table, pos, T, count=None, dtype=torch.float16, out=None):
+    """(k, v) [rows][T][heads * dh] of `dtype` (float32, float16, bfloat16): what a 4-bit cache holds of
+    tokens pos[r] .. pos[r] + count[r] - 1 (None: T of them) of each row, zeros where it holds none.
+    out: (k, v) to write."""
+    kp = pages[0]
+    dev = _dev(kp, "kp")
+    kp, vp, ks, vs, n, H, dh = _pages4(pages, dev)
+    rows = table.shape[0]
+    W = _table(table, rows, dev)
+    _want(pos, "pos", _I32, dev, (rows,), True)
+    if count is not None:
+        _want(count, "count", _I32, dev, (rows,), True)
+    if dtype not in _DT:
+        raise ValueError("dtype must be float32, float16 or bfloat16")
+    if out is None:
+        out = tuple(torch.empty((rows, T, H * dh), dtype=dtype, device=kp.device) for _ in "kv")
+    k, v = out
+    _want(k, "out[0]", (dtype,), dev, (rows, T, H * dh))
+    _want(v, "out[1]", (dtype,), dev, (rows, T, H * dh))
+    (ldk, kr), (ldv, vr) = _strides3(k, "out[0]"), _strides3(v, "out[1]")
+    if T < 2:
+        ldk = ldv = H * dh
+    _call("nv_op_kv4_read", dev, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n,
+          table.data_ptr(), W, pos.data_ptr(), _at(count), rows, T, H, dh, k.data_ptr(), ldk, kr,
+          v.data_ptr(), ldv, vr, _DT[dtype])
+    return k, v
+
+
+def nv_op_attention_kv4_workspace(rows, S, heads, kv_heads, dh, table_w):
+    return int(N.lib.nv_op_attention_kv4_workspace(rows, S, heads, kv_heads, dh, table_w))
+
+
+def nv_op_attention_kv4(q, pages, table, lens, scale, qpos=None, out=None, ws=None):
+    """Multi-head attention of q [rows][S][heads * dh] (float16, bfloat16) over the first lens[r]
+    tokens of each row in a 4-bit cache; with qpos (int32 [rows]) query i of row r sees tokens up to
+    qpos[r] + i.  Query heads share the cache's heads in equal groups.  ws: (owner, address,
+    bytes) of nv_op_attention_kv4_workspace(...) bytes, or None: one for this call."""
+    return _attention(q, _pages4(pages, _dev(q, "q")), table, lens, scale, qpos, out, ws,
+                      "nv_op_attention_kv4")
 
 
 def nv_trace_enable(family_mask, max_launches=65536):

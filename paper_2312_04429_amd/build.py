@@ -14,7 +14,7 @@ OUT_DIR = os.environ.get("NV_BUILD_DIR") or os.path.join(HERE, "_build")
 LIB = os.environ.get("NV_BUILD_OUT") or os.path.join(HERE, "libnv.so")
 SOURCES = ["lookup.hip", "gemm.hip", "attention.hip", "ops.hip", "unet.hip", "trace.hip",
            "probe.hip", "pool.hip", "lcbfu.cpp", "predictor.hip", "ivf.hip", "quant8.hip",
-           "linear8.hip", "kv8.hip"]
+           "linear8.hip", "kv8.hip", "kv4.hip", "rope.hip"]
 ARCH = os.environ.get("NV_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -23,7 +23,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Wno-pass-failed"]
 
 
-# Per-source flags.  attention.hip, kv8.hip: matrix instructions write VGPRs (their
+# Per-source flags.  attention.hip, kv8.hip, kv4.hip: matrix instructions write VGPRs (their
 # softmax reads every score back; the accumulator-register form adds a copy
 # per score).  probe.hip: the same form, which is what reaches the matrix
 # cores' rate in a pure multiply loop (about 2.2 PFLOP/s against 1.2 with
@@ -32,6 +32,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # round exactly as written.
 EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "kv4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "probe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "predictor.hip": ["-ffp-contract=off"],
          "ivf.hip": ["-ffp-contract=off"]}

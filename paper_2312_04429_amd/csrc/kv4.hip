@@ -1,0 +1,496 @@
+// Keys and values kept in 4 bits: appending tokens to their pages, reading them back, and attention
+// over them.
+//
+// Page: 64 tokens of one sequence, keys and values alike [head][64][dh / 2] bytes of two e2m1 codes and
+// [head][64][ceil(dh / 32)] scale bytes.  A token's codes and scales are bytes of its own, so tokens are
+// written in any order and over again without touching others.
+#include <algorithm>
+
+#include "common.h"
+#include "e2m1.h"
+#include "kv4.h"
+#include "kv_join.h"
+
+namespace nv {
+namespace {
+
+constexpr int PAGE = NV_KV4_PAGE;
+constexpr float LOG2E = 1.4426950408889634f;
+
+__host__ __device__ constexpr int blocks_of(int dh) { return (dh + KV4_BLOCK - 1) / KV4_BLOCK; }
+
+// The place of token t of a call's row: unit page * heads + head, times 64, plus the token's slot in the
+// page; -1: not held, or not asked for.
+template <typename Args>
+__device__ __forceinline__ int64_t place_of(const Args& a, int64_t row, int t, int head) {
+  const int64_t pos = a.pos[row];
+  const int cnt = a.count ? std::min(std::max(a.count[row], 0), a.T) : a.T;
+  const int64_t p = (pos + t) / PAGE;
+  if (pos < 0 || t >= cnt || p >= a.table_w) return -1;
+  const int64_t page = a.table[row * a.table_w + p];
+  if (page < 0 || page >= a.n_pages) return -1;
+  return (page * a.heads + head) * PAGE + (pos + t) % PAGE;
+}
+
+// ------------------------------------------------------------------------------------ append
+
+// Four lanes a block of 32 channels, eight channels each.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
+  const bool is_v = blockIdx.z;
+  const int64_t row = blockIdx.y;
+  const int nb = blocks_of(a.dh), lanes = a.heads * nb * 4;  // of a token
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = id / lanes;
+  const int u = (int)(id - t * lanes), head = u / (nb * 4), c = (u - head * nb * 4) * 8;
+  const int64_t at = t < a.T ? place_of(a, row, (int)t, head) : -1;
+  const bool on = at >= 0 && c < a.dh;
+  float x[8];
+  const T* src = (const T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) +
+                 t * (is_v ? a.ldv : a.ldk) + (int64_t)head * a.dh;
+  load8<VEC>(src, c, on ? a.dh : 0, x);
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, abs_or_inf(x[j]));
+  top = fmaxf(top, dpp_f<0xB1>(top));  // quad_perm [1, 0, 3, 2]
+  top = fmaxf(top, dpp_f<0x4E>(top));  // quad_perm [2, 3, 0, 1]
+  if (!on) return;
+  const int e = scale_byte4(top);
+  *(uint32_t*)((is_v ? a.vp : a.kp) + at * (a.dh / 2) + c / 2) =
+      e == 255 ? 0u : codes4x8(x, scale_inverse(e));
+  if (c % KV4_BLOCK == 0) (is_v ? a.vs : a.ks)[at * nb + c / KV4_BLOCK] = (uint8_t)e;
+}
+
+// -------------------------------------------------------------------------------------- read
+
+// Eight channels a lane.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) kv4_read_k(Kv4ReadArgs a) {
+  const bool is_v = blockIdx.z;
+  const int64_t row = blockIdx.y;
+  const int nb = blocks_of(a.dh), nch = a.dh / 8, lanes = a.heads * nch;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = id / lanes;
+  if (t >= a.T) return;
+  const int u = (int)(id - t * lanes), head = u / nch, c = (u - head * nch) * 8;
+  const int64_t at = place_of(a, row, (int)t, head);
+  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (at >= 0) {
+    const uint32_t w = *(const uint32_t*)((is_v ? a.vp : a.kp) + at * (a.dh / 2) + c / 2);
+    const float s = scale_value((is_v ? a.vs : a.ks)[at * nb + c / KV4_BLOCK]);
+    const half8 v = Half8<_Float16>::of(w, 1.f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (float)v[j] * s;
+  }
+  T* to = (T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) + t * (is_v ? a.ldv : a.ldk) +
+          (int64_t)head * a.dh;
+  store8<VEC>(to, c, a.dh, x);
+}
+
+// --------------------------------------------------------------------------------- attention
+//
+// S^T = K Q^T is computed, so an accumulator entry's column is a query and the softmax state is a
+// lane's own; accumulators of two 16-token tiles are then the second product's operand as they stand,
+// against values of the same tokens.
+
+// Head dimension in 32-wide steps; lane group kc takes the 8 STEPS channels from 8 STEPS kc on, so
+// that its codes of a token are neighbours.
+template <int DH>
+struct Dims {
+  static constexpr int STEPS = (DH + 31) / 32, NB = blocks_of(DH), DV = (DH + 15) / 16;
+  static __device__ __forceinline__ int dim(int step, int kc) { return kc * 8 * STEPS + step * 8; }
+};
+
+// Pages p0 .. p1 - 1 of share `split` of a tile's pages: equal parts of at least KV8_SHARE pages, so a
+// short row's last shares may be empty.
+__device__ __forceinline__ void share_of(int pages, int split, int splits, int* p0, int* p1) {
+  const int n = std::max(KV8_SHARE, (pages + splits - 1) / splits);
+  *p0 = (int)std::min<int64_t>((int64_t)split * n, pages);
+  *p1 = std::min(*p0 + n, pages);
+}
+
+// One wave's running softmax over 16 queries: reference (probabilities are 2^(score - m)), their sum,
+// accumulators O^T.
+template <int DH>
+struct State {
+  float m, l;
+  floatx4 acc[Dims<DH>::DV];
+};
+
+// The largest probability is at most 2^P_TOP, which float16 holds.
+constexpr float P_TOP = 15.f;
+
+// The reference under which a score of `top` has the probability 2^room (room <= P_TOP): top - room, or
+// top itself where the scores are so large that this rounds to more than P_TOP below it.
+__device__ __forceinline__ float reference(float top, float room) {
+  const float low = top - room;
+  return top - low > P_TOP ? top : low;
+}
+
+// x as the sum of two bfloat16 numbers: 16 bits of it, and float16 exactly.
+__device__ __forceinline__ void split_bf16(float x, __bf16* hi, __bf16* lo) {
+  *hi = (__bf16)x;
+  const float d = x - (float)*hi;
+  *lo = (__bf16)(d - d == 0.f ? d : 0.f);  // not finite: all of it is in hi
+}
+
+// A page's 64 tokens into the state, whatever is in it: bfloat16 operands, which hold every code times
+// every scale; float16 queries, and probabilities, as sums of two.  Everything comes from global memory
+// as it is needed.  j0: the page's first token; lim: tokens this lane's query sees; len: tokens of
+// the sequence.  A NaN block of values reaches the queries that see its token, in its 32 channels.
+template <typename T, int DH>
+__device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>::Vec* fq,
+                                         const Kv4AttnArgs& a, int64_t ph, float scale2, int j0,
+                                         int lim, int len, int li, int kc) {
+  using D = Dims<DH>;
+  using B = Half8<__bf16>;
+  const uint8_t *kp = a.kp + ph * PAGE * (DH / 2), *ks = a.ks + ph * PAGE * D::NB;
+  const uint8_t *vp = a.vp + ph * PAGE * (DH / 2), *vs = a.vs + ph * PAGE * D::NB;
+  floatx4 s[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const int tok = 16 * t + li;
+#pragma unroll
+    for (int b = 0; b < D::STEPS; ++b) {
+      const int d = D::dim(b, kc);
+      bf16x8 k = {}, qh, ql;
+      if (d < DH) {
+        const int e = ks[tok * D::NB + d / KV4_BLOCK];
+        k = B::of(*(const uint32_t*)(kp + (tok * DH + d) / 2), scale_value(e == 255 ? 127 : e));
+        if (e == 255) k = __builtin_bit_cast(bf16x8, u32x4{0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0});
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __bf16 hi, lo;
+        split_bf16((float)fq[b][i], &hi, &lo);
+        qh[i] = hi, ql[i] = lo;
+      }
+      s[t] = B::mul(k, qh, s[t]);
+      if (std::is_same<T, _Float16>::value) s[t] = B::mul(k, ql, s[t]);
+    }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[t][r] *= scale2;
+      if (j0 + 16 * t + 4 * kc + r >= lim) s[t][r] = -INFINITY;
+      top = fmaxf(top, s[t][r]);
+    }
+  const float mnew = fmaxf(st.m, reference(rows_max(top), P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
+  const float alpha = __builtin_amdgcn_exp2f(st.m - base);
+  st.m = mnew;
+  float sum = 0.f;
+  bf16x8 ph8[2], pl8[2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float p = __builtin_amdgcn_exp2f(s[t][r] - base);
+      __bf16 hi, lo;
+      split_bf16(p, &hi, &lo);
+      ph8[t >> 1][(t & 1) * 4 + r] = hi, pl8[t >> 1][(t & 1) * 4 + r] = lo;
+      sum += (float)hi + (float)lo;
+    }
+  st.l = st.l * alpha + rows_sum(sum);
+  float nan[D::NB];
+#pragma unroll
+  for (int b = 0; b < D::NB; ++b) {
+    nan[b] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int tok = 16 * t + 4 * kc + r;
+        if (j0 + tok < lim && vs[tok * D::NB + b] == 255) nan[b] = 1.f;
+      }
+    nan[b] = rows_max(nan[b]);
+  }
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) {
+    const int c = 16 * j + li;
+    st.acc[j] *= alpha;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int tok = 32 * h + 4 * kc + (i < 4 ? i : i + 12);
+        v[i] = (__bf16)0.f;
+        if (j0 + tok < len && c < DH) {
+          const int e = vs[tok * D::NB + c / KV4_BLOCK];
+          const uint32_t w = vp[(tok * DH + c) / 2];
+          const bf16x2 two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_value(e), 0);
+          if (e != 255) v[i] = two[c & 1];
+        }
+      }
+      st.acc[j] = B::mul(v, ph8[h], st.acc[j]);
+      st.acc[j] = B::mul(v, pl8[h], st.acc[j]);
+    }
+    if (nan[j / 2] != 0.f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.acc[j][r] = __int_as_float(0x7FC00000);
+  }
+}
+
+// A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
+// share of the row's pages, dealt out to its four waves; their states meet in LDS.  With more
+// than one share the means go to the workspace and attn_join_k adds them in order.
+template <typename T, int DH>
+__global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
+  using D = Dims<DH>;
+  typedef typename Half8<T>::Vec Vec;
+  constexpr int NW = 4, CH = D::DV * 16;
+  __shared__ float sm[NW][16], sl[NW][16];
+  __shared__ __align__(16) float so[NW][16][CH + 4];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int id = blockIdx.x;
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int ct = id % a.col_tiles;
+  id /= a.col_tiles;
+  const int head = id % a.kv_heads, row = id / a.kv_heads;
+  const int group = a.heads / a.kv_heads, cols = a.S * group, c0 = ct * 16;
+  const int col = std::min(c0 + li, cols - 1), qs = col / group, qh = head * group + col % group;
+  const int len = (int)std::min<int64_t>(std::max(a.lens[row], 0), (int64_t)a.table_w * PAGE);
+  const int64_t q0 = a.qpos ? (int64_t)a.qpos[row] + 1 : len;  // tokens that query 0 sees
+  auto sees = [&](int s) {
+    return (int)std::max<int64_t>(0, std::min<int64_t>(len, a.qpos ? q0 + s : len));
+  };
+  const int lim = sees(qs);
+  const int most = sees((std::min(c0 + 16, cols) - 1) / group);
+  int p0, p1;
+  share_of((most + PAGE - 1) / PAGE, split, a.splits, &p0, &p1);
+
+  Vec fq[D::STEPS];
+  const T* qrow = (const T*)a.q + (int64_t)row * a.q_row + (int64_t)qs * a.ldq + (int64_t)qh * DH;
+#pragma unroll
+  for (int b = 0; b < D::STEPS; ++b) {
+    const int d = D::dim(b, kc);
+    fq[b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
+  }
+  State<DH> st;
+  st.m = -INFINITY, st.l = 0.f;
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) st.acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const float scale2 = a.scale * LOG2E;
+  const int32_t* table = a.table + (int64_t)row * a.table_w;
+  for (int p = p0 + wave; p < p1; p += NW) {
+    const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
+    if (page < 0 || page >= a.n_pages) continue;
+    page_any<T, DH>(st, fq, a, page * a.kv_heads + head, scale2, p * PAGE, lim, len, li, kc);
+  }
+  // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
+  // sum in its final size may pass float32 where the mean does not).
+  const float l = st.l, mean = l == 0.f ? 0.f : 1.f / l;
+  if (kc == 0) sm[wave][li] = st.m, sl[wave][li] = l;
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j) *(floatx4*)&so[wave][li][j * 16 + kc * 4] = st.acc[j] * mean;
+  __syncthreads();
+  for (int i = tid; i < 16 * (CH / 4); i += 256) {
+    const int c = i / (CH / 4), d = i % (CH / 4) * 4;
+    if (c0 + c >= cols || d >= DH) continue;
+    float m = sm[0][c];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sm[w][c]);
+    const float base = m == -INFINITY ? 0.f : m;
+    float f[NW], ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) ls += f[w] = __builtin_amdgcn_exp2f(sm[w][c] - base) * sl[w][c];
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) o += f[w] * inv * *(const floatx4*)&so[w][c][d];
+    if (a.splits == 1) {
+      const int qi = (c0 + c) / group, h = head * group + (c0 + c) % group;
+      struct alignas(8) Quad { T v[4]; } out;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)o[r];
+      *(Quad*)((T*)a.out + (int64_t)row * a.o_row + (int64_t)qi * a.ldo + (int64_t)h * DH + d) = out;
+    } else {
+      const int64_t slot = (((int64_t)row * a.kv_heads + head) * cols + c0 + c) * a.splits + split;
+      if (m != -INFINITY || ls != 0.f) *(floatx4*)(a.part_o + slot * DH + d) = o;
+      if (d == 0) a.part_ml[slot * 2] = m, a.part_ml[slot * 2 + 1] = ls;
+    }
+  }
+}
+
+template <typename T, int DH>
+hipError_t attn_go(const Kv4AttnArgs& a, hipStream_t s) {
+  const int64_t wgs = (int64_t)a.rows * a.kv_heads * a.col_tiles * a.splits;
+  hipLaunchKernelGGL((attn_kv4_k<T, DH>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  attn_join<T>(a, s);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attn_launch_t(const Kv4AttnArgs& a, hipStream_t s) {
+  switch (a.dh) {
+    case 16: return attn_go<T, 16>(a, s);
+    case 32: return attn_go<T, 32>(a, s);
+    case 40: return attn_go<T, 40>(a, s);
+    case 64: return attn_go<T, 64>(a, s);
+    case 80: return attn_go<T, 80>(a, s);
+    case 128: return attn_go<T, 128>(a, s);
+    case 160: return attn_go<T, 160>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+bool head_dim_ok(int dh) {
+  return dh == 16 || dh == 32 || dh == 40 || dh == 64 || dh == 80 || dh == 128 || dh == 160;
+}
+
+// What append and read check alike.  NV_OK, or the error that is set.
+int32_t check_tokens(int32_t dtype, bool f32, int32_t rows, int32_t T, int32_t heads, int32_t dh,
+                     int64_t n_pages, int32_t table_w, int64_t ldk, int64_t k_row, int64_t ldv,
+                     int64_t v_row, int64_t lanes) {
+  NV_CHECK_ARG(rows >= 0 && rows <= 65535 && T >= 0 && heads >= 1 && heads <= 32767,
+               "need 0 <= rows <= 65535, T >= 0 and 1 <= heads <= 32767");
+  NV_CHECK_ARG(dtype == NV_F16 || dtype == NV_BF16 || (f32 && dtype == NV_F32),
+               f32 ? "dtype must be NV_F32, NV_F16 or NV_BF16" : "dtype must be NV_F16 or NV_BF16");
+  NV_CHECK_ARG(n_pages >= 0 && table_w >= 0, "negative sizes");
+  NV_CHECK_ARG(ldk >= 0 && ldv >= 0 && k_row >= 0 && v_row >= 0, "negative strides");
+  if (!head_dim_ok(dh)) {
+    set_error("dh must be 16, 32, 40, 64, 80, 128 or 160");
+    return NV_ERR_UNSUPPORTED;
+  }
+  if ((int64_t)T * heads * lanes > 0xFFFFFF00ll) {  // threads of a grid's first dimension
+    set_error("more tokens of a row than a grid holds");
+    return NV_ERR_UNSUPPORTED;
+  }
+  return NV_OK;
+}
+
+}  // namespace
+}  // namespace nv
+
+using namespace nv;
+
+extern "C" int32_t nv_op_kv4_append(const void* k, int64_t ldk, int64_t k_row_stride, const void* v,
+                                    int64_t ldv, int64_t v_row_stride, int32_t dtype, int32_t rows,
+                                    int32_t T, int32_t heads, int32_t dh, void* kp, void* vp,
+                                    uint8_t* ks, uint8_t* vs, int64_t n_pages,
+                                    const int32_t* table, int32_t table_w, const int32_t* pos,
+                                    const int32_t* count, void* stream) {
+  clear_error();
+  const int64_t lanes = 4 * blocks_of(std::max(dh, 1));
+  const int32_t st = check_tokens(dtype, false, rows, T, heads, dh, n_pages, table_w, ldk,
+                                  k_row_stride, ldv, v_row_stride, lanes);
+  if (st != NV_OK) return st;
+  if (rows == 0 || T == 0 || n_pages == 0 || table_w == 0) return NV_OK;
+  NV_CHECK_ARG(k && v && kp && vp && ks && vs && table && pos, "null pointer argument");
+  NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
+  const Kv4AppendArgs a{k, v, (uint8_t*)kp, (uint8_t*)vp, ks, vs,
+                        ldk, k_row_stride, ldv, v_row_stride, n_pages, table, pos, count,
+                        T, heads, dh, table_w};
+  const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
+  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows, 2);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+  };
+  if (dtype == NV_F16) vec ? go(kv4_append_k<_Float16, true>) : go(kv4_append_k<_Float16, false>);
+  else vec ? go(kv4_append_k<__bf16, true>) : go(kv4_append_k<__bf16, false>);
+  NV_LAUNCH_CHECK("kv4_append_k");
+  return NV_OK;
+}
+
+extern "C" int32_t nv_op_kv4_read(const void* kp, const void* vp, const uint8_t* ks,
+                                  const uint8_t* vs, int64_t n_pages, const int32_t* table,
+                                  int32_t table_w, const int32_t* pos, const int32_t* count,
+                                  int32_t rows, int32_t T, int32_t heads, int32_t dh, void* k,
+                                  int64_t ldk, int64_t k_row_stride, void* v, int64_t ldv,
+                                  int64_t v_row_stride, int32_t dtype, void* stream) {
+  clear_error();
+  const int64_t lanes = std::max(dh, 0) / 8;
+  const int32_t st = check_tokens(dtype, true, rows, T, heads, dh, n_pages, table_w, ldk,
+                                  k_row_stride, ldv, v_row_stride, lanes);
+  if (st != NV_OK) return st;
+  NV_CHECK_ARG(ldk >= (int64_t)heads * dh && ldv >= (int64_t)heads * dh,
+               "rows of an output shorter than heads * dh");
+  if (rows == 0 || T == 0) return NV_OK;
+  NV_CHECK_ARG(k && v && pos && (table_w == 0 || table) && (n_pages == 0 || (kp && vp && ks && vs)),
+               "null pointer argument");
+  NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
+  const Kv4ReadArgs a{(const uint8_t*)kp, (const uint8_t*)vp, ks, vs, n_pages, table, pos, count,
+                      k, v, ldk, k_row_stride, ldv, v_row_stride, T, heads, dh, table_w};
+  const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
+  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows, 2);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+  };
+  if (dtype == NV_F32) vec ? go(kv4_read_k<float, true>) : go(kv4_read_k<float, false>);
+  else if (dtype == NV_F16) vec ? go(kv4_read_k<_Float16, true>) : go(kv4_read_k<_Float16, false>);
+  else vec ? go(kv4_read_k<__bf16, true>) : go(kv4_read_k<__bf16, false>);
+  NV_LAUNCH_CHECK("kv4_read_k");
+  return NV_OK;
+}
+
+extern "C" size_t nv_op_attention_kv4_workspace(int32_t rows, int32_t S, int32_t heads,
+                                                int32_t kv_heads, int32_t dh, int32_t table_w) {
+  if (rows < 1 || S < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads || !head_dim_ok(dh) ||
+      table_w < 0)
+    return 0;
+  return part_bytes(kv4_plan(rows, S, heads, kv_heads, dh, table_w), rows, S, heads, dh,
+                    nullptr);
+}
+
+extern "C" int32_t nv_op_attention_kv4(const void* q, int64_t ldq, int64_t q_row_stride,
+                                       int32_t dtype, const void* kp, const void* vp,
+                                       const uint8_t* ks, const uint8_t* vs, int64_t n_pages,
+                                       const int32_t* table, int32_t table_w, const int32_t* lens,
+                                       const int32_t* qpos, int32_t rows, int32_t S, int32_t heads,
+                                       int32_t kv_heads, int32_t dh, float scale, void* out,
+                                       int64_t ldo, int64_t o_row_stride, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  clear_error();
+  NV_CHECK_ARG(rows >= 0 && S >= 0 && heads >= 1 && kv_heads >= 1 && heads % kv_heads == 0,
+               "need rows, S >= 0 and heads a positive multiple of kv_heads");
+  NV_CHECK_ARG(dtype == NV_F16 || dtype == NV_BF16, "dtype must be NV_F16 or NV_BF16");
+  NV_CHECK_ARG(n_pages >= 0 && table_w >= 0 && table_w <= 0x7FFFFFFF / PAGE,
+               "need n_pages >= 0 and 0 <= table_w < 2^25");
+  NV_CHECK_ARG(scale - scale == 0.f, "scale must be finite");
+  if (!head_dim_ok(dh)) {
+    set_error("dh must be 16, 32, 40, 64, 80, 128 or 160");
+    return NV_ERR_UNSUPPORTED;
+  }
+  NV_CHECK_ARG(ldq >= 0 && q_row_stride >= 0 && ldo >= (int64_t)heads * dh && o_row_stride >= 0,
+               "negative strides, or rows of out shorter than heads * dh");
+  if (rows == 0 || S == 0) return NV_OK;
+  NV_CHECK_ARG(q && lens && out && (table_w == 0 || table) &&
+                   (n_pages == 0 || (kp && vp && ks && vs)), "null pointer argument");
+  if ((ldq | q_row_stride | ldo | o_row_stride) % 8 || !aligned16(q) || !aligned16(out)) {
+    set_error("q and out need 16-byte aligned buffers and strides in multiples of 8");
+    return NV_ERR_UNSUPPORTED;
+  }
+  NV_CHECK_ARG(aligned16(kp) && aligned16(vp), "kp and vp must be 16-byte aligned");
+  const Kv8Plan p = kv4_plan(rows, S, heads, kv_heads, dh, table_w);
+  if ((int64_t)S * (heads / kv_heads) > 0x7FFFFFF0 ||
+      (double)rows * kv_heads * p.col_tiles * p.splits > 8388607.0) {
+    set_error("more queries than a grid holds");
+    return NV_ERR_UNSUPPORTED;
+  }
+  size_t ml_at = 0;
+  const size_t need = part_bytes(p, rows, S, heads, dh, &ml_at);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))) {
+    set_error("workspace missing, misaligned or smaller than nv_op_attention_kv4_workspace()");
+    return NV_ERR_WORKSPACE;
+  }
+  Kv4AttnArgs a{};
+  a.q = q, a.ldq = ldq, a.q_row = q_row_stride;
+  a.kp = (const uint8_t*)kp, a.vp = (const uint8_t*)vp, a.ks = ks, a.vs = vs;
+  a.n_pages = n_pages, a.table = table, a.table_w = table_w, a.lens = lens, a.qpos = qpos;
+  a.rows = rows, a.S = S, a.heads = heads, a.kv_heads = kv_heads, a.dh = dh, a.scale = scale;
+  a.out = out, a.ldo = ldo, a.o_row = o_row_stride;
+  a.col_tiles = p.col_tiles, a.splits = p.splits, a.tall = p.tall;
+  if (need) {
+    a.part_o = (float*)workspace;
+    a.part_ml = (float*)((uint8_t*)workspace + ml_at);
+  }
+  const hipStream_t s = (hipStream_t)stream;
+  NV_HIP_TRY(dtype == NV_F16 ? attn_launch_t<_Float16>(a, s) : attn_launch_t<__bf16>(a, s));
+  return NV_OK;
+}
