@@ -144,6 +144,8 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
                                          int lim, int len, int li, int kc) {
   using D = Dims<DH>;
   using B = Half8<__bf16>;
+  // Nothing of this is to be computed ahead of a loop over pages and kept in registers there.
+  asm volatile("" : "+v"(li), "+v"(kc));
   const uint8_t *kp = a.kp + ph * PAGE * (DH / 2), *ks = a.ks + ph * PAGE * D::NB;
   const uint8_t *vp = a.vp + ph * PAGE * (DH / 2), *vs = a.vs + ph * PAGE * D::NB;
   floatx4 s[4];
@@ -155,6 +157,8 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
     for (int b = 0; b < D::STEPS; ++b) {
       const int d = D::dim(b, kc);
       bf16x8 k = {}, qh, ql;
+      auto fb = fq[b];
+      asm volatile("" : "+v"(fb));
       if (d < DH) {
         const int e = ks[tok * D::NB + d / KV4_BLOCK];
         k = B::of(*(const uint32_t*)(kp + (tok * DH + d) / 2), scale_value(e == 255 ? 127 : e));
@@ -163,11 +167,12 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __bf16 hi, lo;
-        split_bf16((float)fq[b][i], &hi, &lo);
+        split_bf16((float)fb[i], &hi, &lo);
         qh[i] = hi, ql[i] = lo;
       }
       s[t] = B::mul(k, qh, s[t]);
       if (std::is_same<T, _Float16>::value) s[t] = B::mul(k, ql, s[t]);
+      __builtin_amdgcn_sched_barrier(0);  // few registers, not speed: this is the rare way
     }
   }
   float top = -INFINITY;
@@ -207,6 +212,7 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
         if (j0 + tok < lim && vs[tok * D::NB + b] == 255) nan[b] = 1.f;
       }
     nan[b] = rows_max(nan[b]);
+    __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) {
@@ -228,11 +234,206 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
       }
       st.acc[j] = B::mul(v, ph8[h], st.acc[j]);
       st.acc[j] = B::mul(v, pl8[h], st.acc[j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
     if (nan[j / 2] != 0.f)
 #pragma unroll
       for (int r = 0; r < 4; ++r) st.acc[j][r] = __int_as_float(0x7FC00000);
   }
+}
+
+// What the kernels below read a page in: units of CW channels of a token, UPT of them a token, for keys
+// and values alike.
+template <int DH>
+struct Units {
+  static constexpr int CW = DH % 32 == 0 ? 32 : DH % 16 == 0 ? 16 : 8, UPT = DH / CW, N = PAGE * UPT;
+  struct Codes { uint32_t w[CW / 8]; };
+  static __device__ __forceinline__ Codes load(const uint8_t* codes, int i) {
+    Codes c;
+    __builtin_memcpy(&c, __builtin_assume_aligned(codes + i * (CW / 2), CW / 2), CW / 2);
+    return c;
+  }
+  static __device__ __forceinline__ int scale(const uint8_t* scales, int i) {
+    return scales[i / UPT * blocks_of(DH) + i % UPT * CW / KV4_BLOCK];
+  }
+};
+
+// Scale bytes whose codes a 16-bit type holds exactly (a block of zeros does with any but 255, but is
+// not asked for here: its codes are).
+template <typename T>
+__device__ __forceinline__ bool exact(int e) {
+  return std::is_same<T, _Float16>::value ? (unsigned)(e - 104) <= 36u : (unsigned)(e - 1) <= 253u;
+}
+template <typename T, int DH>
+__device__ __forceinline__ bool exact(int e, const typename Units<DH>::Codes& c) {
+  if (exact<T>(e)) return true;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < Units<DH>::CW / 8; ++i) any |= c.w[i];
+  return e != 255 && (any & 0x77777777u) == 0;
+}
+__device__ __forceinline__ float scale_bits(int e) { return __int_as_float(e << 23); }
+
+// A page's values in LDS, token after token in float16; a row is an odd number of 32-byte steps, so that
+// the 16 rows of a transposed read lie in different banks.
+template <int DH>
+struct Values {
+  static constexpr int ROW = (Dims<DH>::DV | 1) == Dims<DH>::DV ? (Dims<DH>::DV + 2) * 16
+                                                                 : (Dims<DH>::DV + 1) * 16;
+  static __device__ __forceinline__ void store(_Float16* to, int i, const typename Units<DH>::Codes& c,
+                                               float scale) {
+    using U = Units<DH>;
+    to += i / U::UPT * ROW + i % U::UPT * U::CW;
+#pragma unroll
+    for (int k = 0; k < U::CW / 8; ++k) *(half8*)(to + k * 8) = Half8<_Float16>::of(c.w[k], scale);
+  }
+  // Channels 16 j + li of tokens 32 h + 4 kc .. + 3 and 16 further: four rows of 16 channels a lane
+  // group, turned on their way (ds_read_b64_tr_b16).
+  static __device__ __forceinline__ half8 load(const _Float16* v, int j, int h, int li, int kc) {
+    typedef __attribute__((ext_vector_type(4))) short Short4;
+    typedef __attribute__((address_space(3))) Short4* Lds;
+    const _Float16* p = v + (32 * h + 4 * kc + (li >> 2)) * ROW + 16 * j + (li & 3) * 4;
+    const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p),
+                 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 16 * ROW));
+    return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// Sums over the 64 keys of a page out of the matrix unit, of the probabilities as rounded: a row of ones.
+__device__ __forceinline__ floatx4 add_probs(const half8* fp, floatx4 sum) {
+  half8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (_Float16)1.f;
+  return Half8<_Float16>::mul(ones, fp[1], Half8<_Float16>::mul(ones, fp[0], sum));
+}
+
+// A lane's part of a page of one head: codes of keys 16 t + li, channels 8 STEPS kc .., and units of
+// values, with their scales.
+template <int DH>
+struct PageCodes {
+  using D = Dims<DH>;
+  using U = Units<DH>;
+  static constexpr bool ONE = 32 % (8 * D::STEPS) == 0;  // a lane's keys have one scale
+  static constexpr int KE = ONE ? 1 : D::STEPS, VU = (U::N + 63) / 64;
+  struct Key { uint32_t w[D::STEPS]; };
+  Key k[4];
+  typename U::Codes v[VU];
+  int ke[4][KE], ve[VU];
+  __device__ __forceinline__ void load_keys(const Kv4AttnArgs& a, int64_t ph, int li, int kc) {
+    const uint8_t *kp = a.kp + ph * PAGE * (DH / 2) + li * (DH / 2) + kc * 4 * D::STEPS,
+                  *ks = a.ks + ph * PAGE * D::NB + li * D::NB;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (DH % 32 == 0) {
+        __builtin_memcpy(&k[t], __builtin_assume_aligned(kp + t * 16 * (DH / 2), 4), sizeof(Key));
+      } else {
+#pragma unroll
+        for (int b = 0; b < D::STEPS; ++b)
+          k[t].w[b] = D::dim(b, kc) < DH ? *(const uint32_t*)(kp + t * 16 * (DH / 2) + b * 4) : 0u;
+      }
+#pragma unroll
+      for (int b = 0; b < KE; ++b)
+        ke[t][b] = D::dim(b, kc) < DH ? ks[t * 16 * D::NB + D::dim(b, kc) / KV4_BLOCK] : 127;
+    }
+  }
+  __device__ __forceinline__ void load_values(const Kv4AttnArgs& a, int64_t ph, int lane) {
+    const uint8_t *vp = a.vp + ph * PAGE * (DH / 2), *vs = a.vs + ph * PAGE * D::NB;
+#pragma unroll
+    for (int i = 0; i < VU; ++i) {
+      v[i] = U::load(vp, i * 64 + lane);
+      ve[i] = U::scale(vs, i * 64 + lane);
+    }
+  }
+  // Scales of tokens from n on become 1: what is there may be anything.
+  __device__ __forceinline__ void cut(int n, int lane, int li) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < KE; ++b)
+        if (16 * t + li >= n) ke[t][b] = 127;
+#pragma unroll
+    for (int i = 0; i < VU; ++i)
+      if ((i * 64 + lane) / U::UPT >= n) ve[i] = 127;
+  }
+  // Whether 16-bit operands hold all of it.
+  template <typename T>
+  __device__ __forceinline__ bool exact16() const {
+    bool ok = true;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < KE; ++b) ok &= exact<T>(ke[t][b]);
+#pragma unroll
+    for (int i = 0; i < VU; ++i) ok &= exact<_Float16>(ve[i]);
+    if (!__ballot(!ok)) return true;
+    ok = true;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int b = 0; b < D::STEPS; ++b) {
+        const int e = ke[t][ONE ? 0 : b];
+        ok &= exact<T>(e) || (e != 255 && (k[t].w[b] & 0x77777777u) == 0);
+      }
+#pragma unroll
+    for (int i = 0; i < VU; ++i) ok &= exact<_Float16, DH>(ve[i], v[i]);
+    return !__ballot(!ok);
+  }
+};
+
+// A page's 64 tokens into the state, in 16-bit operands that hold them.  lim: tokens this lane's query
+// sees; some: whether some query sees only part of the page.  keys_done and values_done run once the
+// keys' and the values' registers are free again.
+template <typename T, int DH, typename KeysDone, typename ValuesDone>
+__device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>::Vec* fq,
+                                          PageCodes<DH>& pc, _Float16* lds, float scale2, int j0,
+                                          int lim, bool some, int lane, int li, int kc,
+                                          KeysDone&& keys_done, ValuesDone&& values_done) {
+  using D = Dims<DH>;
+  using M = Half8<T>;
+  using PC = PageCodes<DH>;
+  floatx4 s[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < D::STEPS; ++b)
+      s[t] = M::mul(M::of(pc.k[t].w[b], scale_bits(pc.ke[t][PC::ONE ? 0 : b])), fq[b], s[t]);
+  }
+  keys_done();
+#pragma unroll
+  for (int i = 0; i < PC::VU; ++i) Values<DH>::store(lds, i * 64 + lane, pc.v[i], scale_bits(pc.ve[i]));
+  values_done();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a wave's LDS is its own
+  float top = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[t][r] *= scale2;
+      if (some && j0 + 16 * t + 4 * kc + r >= lim) s[t][r] = -INFINITY;
+      top = fmaxf(top, s[t][r]);
+    }
+  const float mnew = fmaxf(st.m, reference(rows_max(top), P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
+  const float alpha = __builtin_amdgcn_exp2f(st.m - base);
+  if (__ballot(mnew != st.m)) {
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) st.acc[j] *= alpha;
+    st.l *= alpha;
+    st.m = mnew;
+  }
+  half8 fp[2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[t][r] - base);
+  st.l += add_probs(fp, floatx4{0.f, 0.f, 0.f, 0.f})[0];
+#pragma unroll
+  for (int j = 0; j < D::DV; ++j)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      st.acc[j] = Half8<_Float16>::mul(Values<DH>::load(lds, j, h, li, kc), fp[h], st.acc[j]);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // A workgroup takes 16 queries of one row and kv head (query heads of the group innermost) and
@@ -243,8 +444,10 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
   using D = Dims<DH>;
   typedef typename Half8<T>::Vec Vec;
   constexpr int NW = 4, CH = D::DV * 16;
+  constexpr int VALS = PAGE * Values<DH>::ROW * 2, OUT = 16 * (CH + 4) * 4;  // bytes of a wave
   __shared__ float sm[NW][16], sl[NW][16];
-  __shared__ __align__(16) float so[NW][16][CH + 4];
+  __shared__ __align__(16) char lds[NW * (VALS > OUT ? VALS : OUT)];
+  float(*so)[16][CH + 4] = (float(*)[16][CH + 4])lds;  // once no wave reads values any more
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int id = blockIdx.x;
@@ -260,7 +463,7 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
   auto sees = [&](int s) {
     return (int)std::max<int64_t>(0, std::min<int64_t>(len, a.qpos ? q0 + s : len));
   };
-  const int lim = sees(qs);
+  const int lim = sees(qs), least = sees(c0 / group);
   const int most = sees((std::min(c0 + 16, cols) - 1) / group);
   int p0, p1;
   share_of((most + PAGE - 1) / PAGE, split, a.splits, &p0, &p1);
@@ -277,12 +480,40 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) st.acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   const float scale2 = a.scale * LOG2E;
+  // The next page's keys are requested as soon as this one's are multiplied, its values once this one's
+  // are in LDS, into the same registers; its table entry was read a page earlier.
   const int32_t* table = a.table + (int64_t)row * a.table_w;
-  for (int p = p0 + wave; p < p1; p += NW) {
-    const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
-    if (page < 0 || page >= a.n_pages) continue;
-    page_any<T, DH>(st, fq, a, page * a.kv_heads + head, scale2, p * PAGE, lim, len, li, kc);
+  int pn = p0 + wave, entry = pn < p1 ? table[pn] : 0;
+  auto take = [&](int& p) {  // page and head of the next page that is there; -1: none left
+    while (pn < p1) {
+      p = pn;
+      const int64_t page = __builtin_amdgcn_readfirstlane(entry);
+      pn += NW;
+      if (pn < p1) entry = table[pn];
+      if (page >= 0 && page < a.n_pages) return page * a.kv_heads + head;
+    }
+    return (int64_t)-1;
+  };
+  _Float16* vals = (_Float16*)(lds + wave * VALS);
+  PageCodes<DH> pc;
+  int p = 0;
+  int64_t ph = take(p);
+  if (ph >= 0) pc.load_keys(a, ph, li, kc), pc.load_values(a, ph, lane);
+  while (ph >= 0) {
+    const int j0 = p * PAGE;
+    const int64_t next = take(p);
+    auto keys = [&] { if (next >= 0) pc.load_keys(a, next, li, kc); };
+    auto values = [&] { if (next >= 0) pc.load_values(a, next, lane); };
+    if (j0 + PAGE > len) pc.cut(len - j0, lane, li);
+    if (pc.template exact16<T>()) {
+      page_step<T, DH>(st, fq, pc, vals, scale2, j0, lim, j0 + PAGE > least, lane, li, kc, keys, values);
+    } else {
+      page_any<T, DH>(st, fq, a, ph, scale2, j0, lim, len, li, kc);
+      keys(), values();
+    }
+    ph = next;
   }
+  __syncthreads();
   // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
   // sum in its final size may pass float32 where the mean does not).
   const float l = st.l, mean = l == 0.f ? 0.f : 1.f / l;
