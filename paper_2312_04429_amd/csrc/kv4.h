@@ -24,15 +24,7 @@ struct Kv4ReadArgs {
 typedef Kv8AttnArgs Kv4AttnArgs;  // kp, vp: bytes of two codes; ks, vs: scale bytes of blocks
 
 inline Kv8Plan kv4_plan(int64_t rows, int S, int heads, int kv_heads, int dh, int table_w) {
-  // products of three sizes are taken in float64: they may pass 64 bits before they are refused
-  const int64_t cols = (int64_t)S * (heads / kv_heads);
-  const double n = (double)(rows * kv_heads) * (double)((cols + 15) / 16);
-  Kv8Plan p{0, 1, 0};
-  if (table_w > 16)
-    p.splits = (int)std::max(1., std::min((n <= 128. ? 256. : 512.) / n, table_w / 4.));
-  p.splits = std::min(p.splits, KV8_MAX_SPLITS);
-  p.col_tiles = (int)std::min<int64_t>((cols + 15) / 16, 0x7FFFFFFF);
-  return p;
+  return kv8_plan(rows, S, heads, kv_heads, dh, table_w);
 }
 
 }  // namespace nv

@@ -549,10 +549,307 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
   }
 }
 
+// Many queries of a head: NW waves of QB * 16 queries share every page.  A page's codes come two
+// pages ahead into registers and are converted once, on their way into a double-buffered LDS
+// (16-bit: the products then read operands as they stand, values turned).  A page that not every query
+// sees whole has its scores masked; one that 16 bits do not hold (or with a NaN) waits until the loop is
+// over and goes through page_any.  Workgroups run in order of falling work under a causal limit: the
+// last queries of every head first, which counts where not all of them are resident at once.
+template <typename T, int DH, int NW, int QB>
+__global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
+  using D = Dims<DH>;
+  using M = Half8<T>;
+  typedef typename M::Vec Vec;
+  using V = Half8<_Float16>;
+  using U = Units<DH>;
+  constexpr int NT = NW * 64, COLS = NW * QB * 16;
+  constexpr int UPL = (2 * U::N + NT - 1) / NT;  // units of keys, then of values, a lane
+  constexpr int KROW = D::STEPS * 32 + 8, VSIZE = PAGE * Values<DH>::ROW;
+  __shared__ __align__(16) T sk[2][PAGE * KROW];
+  __shared__ __align__(16) _Float16 sv[2][VSIZE];
+  __shared__ int waits[2];  // page + 1 of the page in a buffer if it waits
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rh = blockIdx.x % (a.rows * a.kv_heads);  // a multiple of 8: one XCD's L2 for a head
+  const int rest = blockIdx.x / (a.rows * a.kv_heads), split = rest / a.col_tiles;
+  const int ct = a.col_tiles - 1 - rest % a.col_tiles;
+  const int head = rh % a.kv_heads, row = rh / a.kv_heads;
+  const int group = a.heads / a.kv_heads, cols = a.S * group, c0 = ct * COLS;
+  const int len = (int)std::min<int64_t>(std::max(a.lens[row], 0), (int64_t)a.table_w * PAGE);
+  const int64_t q0 = a.qpos ? (int64_t)a.qpos[row] + 1 : len;  // tokens that query 0 sees
+  auto sees = [&](int c) {                                     // tokens that column c sees
+    c = std::min(c, cols - 1) / group;
+    return (int)std::max<int64_t>(0, std::min<int64_t>(len, a.qpos ? q0 + c : len));
+  };
+  const int32_t* table = a.table + (int64_t)row * a.table_w;
+  const float scale2 = a.scale * LOG2E;
+
+  Vec fq[QB][D::STEPS];
+  State<DH> st[QB];
+  floatx4 sum[QB];  // of a lane's query, four times
+  int lim[QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int col = std::min(c0 + (wave * QB + qb) * 16 + li, cols - 1);
+    lim[qb] = sees(col);
+    const T* qrow = (const T*)a.q + (int64_t)row * a.q_row + (int64_t)(col / group) * a.ldq +
+                    (int64_t)(head * group + col % group) * DH;
+#pragma unroll
+    for (int b = 0; b < D::STEPS; ++b) {
+      const int d = D::dim(b, kc);
+      fq[qb][b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
+    }
+    st[qb].m = -INFINITY, sum[qb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) st[qb].acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  struct Page { int64_t ph; int p; };
+  int pnext, pages;  // the next page of this share, and its end
+  share_of((sees(c0 + COLS - 1) + PAGE - 1) / PAGE, split, a.splits, &pnext, &pages);
+  const int first = pnext;
+  const int wave_least = sees(c0 + wave * QB * 16), wave_most = sees(c0 + (wave + 1) * QB * 16 - 1);
+  // The next page that is there (p.ph < 0: none left).  Its table entry was read at the last call:
+  // the page's address does not wait for memory.
+  int entry = pnext < pages ? table[pnext] : 0;
+  auto take = [&](Page& p) {
+    p.ph = -1;
+    while (pnext < pages) {
+      const int64_t page = __builtin_amdgcn_readfirstlane(entry);
+      p.p = pnext++;
+      if (pnext < pages) entry = table[pnext];
+      if (page < 0 || page >= a.n_pages) continue;
+      p.ph = page * a.kv_heads + head;
+      break;
+    }
+  };
+  typename U::Codes code[UPL];
+  int sc[UPL];
+  auto fetch = [&](const Page& p) {
+#pragma unroll
+    for (int i = 0; i < UPL; ++i) {
+      const int u = i * NT + tid;
+      if (2 * U::N % NT != 0 && u >= 2 * U::N) break;  // whole waves
+      const bool is_v = u >= U::N;
+      const int n = is_v ? u - U::N : u;
+      code[i] = U::load((is_v ? a.vp : a.kp) + p.ph * PAGE * (DH / 2), n);
+      sc[i] = U::scale((is_v ? a.vs : a.ks) + p.ph * PAGE * D::NB, n);
+    }
+  };
+  auto stash = [&](const Page& p, int buf) {
+    const int n = len - p.p * PAGE;
+#pragma unroll
+    for (int i = 0; i < UPL; ++i) {
+      const int u = i * NT + tid;
+      if (2 * U::N % NT != 0 && u >= 2 * U::N) break;
+      const bool is_v = u >= U::N;
+      const int w = is_v ? u - U::N : u, tok = w / U::UPT;
+      int e = sc[i];
+      if (n < PAGE && tok >= n) e = 127;  // what is behind the sequence may be anything
+      if (is_v) {
+        if (!exact<_Float16, DH>(e, code[i])) waits[buf] = p.p + 1;
+        Values<DH>::store(sv[buf], w, code[i], scale_bits(e));
+      } else {
+        if (!exact<T, DH>(e, code[i])) waits[buf] = p.p + 1;
+        T* to = sk[buf] + tok * KROW + w % U::UPT * U::CW;
+#pragma unroll
+        for (int k = 0; k < U::CW / 8; ++k) *(Vec*)(to + k * 8) = M::of(code[i].w[k], scale_bits(e));
+      }
+    }
+  };
+
+  auto attend = [&](int buf, int j0, bool some) {
+    const T* K_ = sk[buf];
+    // Key fragments are requested TG tiles at a time, VG tiles of values before the softmax, whose
+    // arithmetic covers their way.
+    constexpr int TG = DH >= 128 ? 2 : 4, VG = DH >= 128 ? D::DV / 2 : D::DV;
+    floatx4 s[QB][4];
+#pragma unroll
+    for (int t0 = 0; t0 < 4; t0 += TG) {
+      Vec fk[TG][D::STEPS];
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int b = 0; b < D::STEPS; ++b) {
+          const int d = D::dim(b, kc);  // past dh: the row's first channels against zeros
+          fk[t][b] = *(const Vec*)(K_ + ((t0 + t) * 16 + li) * KROW + (d < DH ? d : 0));
+        }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int b = 0; b < D::STEPS; ++b)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            s[qb][t0 + t] =
+                M::mul(fk[t][b], fq[qb][b], b ? s[qb][t0 + t] : floatx4{0.f, 0.f, 0.f, 0.f});
+    }
+    half8 fv[VG][2];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < VG; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) fv[j][h] = Values<DH>::load(sv[buf], j, h, li, kc);
+    __builtin_amdgcn_sched_barrier(0);
+    // Scores relative to the query's reference.  It moves only when a probability would pass 2^P_TOP,
+    // and then to where the largest is 2^LOW: low enough that few pages move it, high enough for what
+    // is small beside it.
+    constexpr float LOW = 9.f;
+    bool grow = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const float base = st[qb].m == -INFINITY ? 0.f : st[qb].m;
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[qb][t][r] = fmaf(s[qb][t][r], scale2, -base);
+          top = fmaxf(top, s[qb][t][r]);
+        }
+      if (some) {  // uniform
+        const int n = lim[qb] - j0 - 4 * kc;
+        top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (16 * t + r >= n) s[qb][t][r] = -INFINITY;
+            top = fmaxf(top, s[qb][t][r]);
+          }
+      }
+      grow |= !(top <= P_TOP) || st[qb].m == -INFINITY;
+    }
+    if (__ballot(grow)) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[qb][t][r]);
+        top = rows_max(top);
+        const bool fresh = st[qb].m == -INFINITY;
+        const float low = reference(top, LOW);
+        const float move = low == -INFINITY ? 0.f : fresh ? low : fmaxf(low, 0.f);
+        const float mnew = fresh ? low : st[qb].m + move;
+        const float alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-move);
+        st[qb].m = mnew;
+        sum[qb] *= alpha;
+#pragma unroll
+        for (int j = 0; j < D::DV; ++j) st[qb].acc[j] *= alpha;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[qb][t] -= move;
+      }
+    }
+    half8 fp[QB][2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          fp[qb][t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[qb][t][r]);
+      sum[qb] = add_probs(fp[qb], sum[qb]);
+    }
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const half8 v = j < VG ? fv[j < VG ? j : 0][h] : Values<DH>::load(sv[buf], j, h, li, kc);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = V::mul(v, fp[qb][h], st[qb].acc[j]);
+      }
+  };
+
+  bool late = false;  // some page waits
+  Page cur, ahead;
+  if (tid < 2) waits[tid] = 0;
+  __syncthreads();
+  take(cur);
+  if (cur.ph >= 0) {
+    fetch(cur);
+    stash(cur, 0);
+    take(ahead);
+    if (ahead.ph >= 0) fetch(ahead);
+    int buf = 0;
+    while (true) {
+      __syncthreads();  // the page is in LDS; the other buffer is read no more
+      const int j0 = cur.p * PAGE;
+      const bool wait = __builtin_amdgcn_readfirstlane(waits[buf]) == cur.p + 1;
+      late |= wait;
+      if (j0 < wave_most && !wait) attend(buf, j0, j0 + PAGE > wave_least);
+      if (ahead.ph < 0) break;
+      stash(ahead, buf ^ 1);
+      cur = ahead;
+      take(ahead);
+      if (ahead.ph >= 0) fetch(ahead);
+      buf ^= 1;
+    }
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) st[qb].l = sum[qb][0];
+  // The pages that wait: the same rule tells which they are.
+  for (int p = first; late && p < pages; ++p) {
+    const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
+    if (page < 0 || page >= a.n_pages) continue;
+    const int64_t ph = page * a.kv_heads + head;
+    bool wait = false;
+    for (int i = lane; i < 2 * U::N; i += 64) {
+      const bool is_v = i >= U::N;
+      const int n = is_v ? i - U::N : i;
+      if (p * PAGE + n / U::UPT >= len) continue;
+      const auto c = U::load((is_v ? a.vp : a.kp) + ph * PAGE * (DH / 2), n);
+      const int e = U::scale((is_v ? a.vs : a.ks) + ph * PAGE * D::NB, n);
+      wait |= is_v ? !exact<_Float16, DH>(e, c) : !exact<T, DH>(e, c);
+    }
+    if (!__ballot(wait)) continue;
+    auto take_in = [&](auto n) {  // (a loop of two would be kept, its state in memory)
+      constexpr int qb = decltype(n)::value;
+      if (__ballot(lim[qb] > p * PAGE))
+        page_any<T, DH>(st[qb], fq[qb], a, ph, scale2, p * PAGE, lim[qb], len, li, kc);
+    };
+    take_in(std::integral_constant<int, 0>());
+    if constexpr (QB > 1) take_in(std::integral_constant<int, 1>());
+  }
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int col = c0 + (wave * QB + qb) * 16 + li;
+    const float l = st[qb].l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (col >= cols) continue;
+    if (a.splits > 1) {
+      const int64_t slot = ((int64_t)rh * cols + col) * a.splits + split;
+#pragma unroll
+      for (int j = 0; j < D::DV; ++j) {
+        const int d = j * 16 + kc * 4;
+        if ((DH % 16 == 0 || d < DH) && (st[qb].m != -INFINITY || l != 0.f))
+          *(floatx4*)(a.part_o + slot * DH + d) = st[qb].acc[j] * inv;
+      }
+      if (kc == 0) a.part_ml[slot * 2] = st[qb].m, a.part_ml[slot * 2 + 1] = l;
+      continue;
+    }
+    T* to = (T*)a.out + (int64_t)row * a.o_row + (int64_t)(col / group) * a.ldo +
+            (int64_t)(head * group + col % group) * DH;
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) {
+      const int d = j * 16 + kc * 4;
+      if (DH % 16 && d >= DH) continue;
+      struct alignas(8) Quad { T v[4]; } out;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out.v[r] = (T)(st[qb].acc[j][r] * inv);
+      *(Quad*)(to + d) = out;
+    }
+  }
+}
+
 template <typename T, int DH>
 hipError_t attn_go(const Kv4AttnArgs& a, hipStream_t s) {
   const int64_t wgs = (int64_t)a.rows * a.kv_heads * a.col_tiles * a.splits;
-  hipLaunchKernelGGL((attn_kv4_k<T, DH>), dim3((unsigned)wgs), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)wgs);
+  if (a.tall == 0) hipLaunchKernelGGL((attn_kv4_k<T, DH>), grid, dim3(256), 0, s, a);
+  else if (a.tall == 1) hipLaunchKernelGGL((attn_kv4_tall_k<T, DH, 4, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attn_kv4_tall_k<T, DH, 4, 2>), grid, dim3(256), 0, s, a);
   attn_join<T>(a, s);
   return hipGetLastError();
 }
