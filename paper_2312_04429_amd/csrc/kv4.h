@@ -24,7 +24,13 @@ struct Kv4ReadArgs {
 typedef Kv8AttnArgs Kv4AttnArgs;  // kp, vp: bytes of two codes; ks, vs: scale bytes of blocks
 
 inline Kv8Plan kv4_plan(int64_t rows, int S, int heads, int kv_heads, int dh, int table_w) {
-  return kv8_plan(rows, S, heads, kv_heads, dh, table_w);
+  Kv8Plan p = kv8_plan(rows, S, heads, kv_heads, dh, table_w);
+  if (p.tall == 0 && table_w > 16) {
+    const double n = (double)(rows * kv_heads) * p.col_tiles;
+    p.splits = (int)std::max(1., std::min(512. / n, table_w / 4.));
+    p.splits = std::min(p.splits, KV8_MAX_SPLITS);
+  }
+  return p;
 }
 
 }  // namespace nv

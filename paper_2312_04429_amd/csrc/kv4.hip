@@ -409,13 +409,22 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      s[t][r] *= scale2;
-      if (some && j0 + 16 * t + 4 * kc + r >= lim) s[t][r] = -INFINITY;
       top = fmaxf(top, s[t][r]);
     }
-  const float mnew = fmaxf(st.m, reference(rows_max(top), P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
-  const float alpha = __builtin_amdgcn_exp2f(st.m - base);
+  if (some) {  // uniform
+    top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (j0 + 16 * t + 4 * kc + r >= lim) s[t][r] = -INFINITY;
+        top = fmaxf(top, s[t][r]);
+      }
+  }
+  const float mnew = fmaxf(st.m, reference(rows_max(top) * scale2, P_TOP)),
+              base = mnew == -INFINITY ? 0.f : mnew;
   if (__ballot(mnew != st.m)) {
+    const float alpha = __builtin_amdgcn_exp2f(st.m - base);
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) st.acc[j] *= alpha;
     st.l *= alpha;
@@ -426,7 +435,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[t][r] - base);
+      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[t][r], scale2, -base));
   st.l += add_probs(fp, floatx4{0.f, 0.f, 0.f, 0.f})[0];
 #pragma unroll
   for (int j = 0; j < D::DV; ++j)
@@ -474,12 +483,16 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
   for (int b = 0; b < D::STEPS; ++b) {
     const int d = D::dim(b, kc);
     fq[b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
+    // the scale's sign to the queries, so that the largest product is the largest score
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      fq[b][i] = a.scale > 0.f ? fq[b][i] : a.scale < 0.f ? -fq[b][i] : fq[b][i] * (T)0.f;
   }
   State<DH> st;
   st.m = -INFINITY, st.l = 0.f;
 #pragma unroll
   for (int j = 0; j < D::DV; ++j) st.acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const float scale2 = a.scale * LOG2E;
+  const float scale2 = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
   // The next page's keys are requested as soon as this one's are multiplied, its values once this one's
   // are in LDS, into the same registers; its table entry was read a page earlier.
   const int32_t* table = a.table + (int64_t)row * a.table_w;
@@ -499,6 +512,7 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
   int p = 0;
   int64_t ph = take(p);
   if (ph >= 0) pc.load_keys(a, ph, li, kc), pc.load_values(a, ph, lane);
+  bool late = false;  // some page waits
   while (ph >= 0) {
     const int j0 = p * PAGE;
     const int64_t next = take(p);
@@ -508,10 +522,22 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
     if (pc.template exact16<T>()) {
       page_step<T, DH>(st, fq, pc, vals, scale2, j0, lim, j0 + PAGE > least, lane, li, kc, keys, values);
     } else {
-      page_any<T, DH>(st, fq, a, ph, scale2, j0, lim, len, li, kc);
+      late = true;
       keys(), values();
     }
     ph = next;
+  }
+  // Pages that 16 bits do not hold, or with a NaN: the same rule tells which they are.  (In the loop above
+  // their code would cost the others a tenth in copies of registers.)
+  for (pn = p0 + wave; late && pn < p1; pn += NW) {
+    const int64_t page = __builtin_amdgcn_readfirstlane(table[pn]);
+    if (page < 0 || page >= a.n_pages) continue;
+    const int j0 = pn * PAGE;
+    pc.load_keys(a, page * a.kv_heads + head, li, kc);
+    pc.load_values(a, page * a.kv_heads + head, lane);
+    pc.cut(len - j0, lane, li);
+    if (!pc.template exact16<T>())
+      page_any<T, DH>(st, fq, a, page * a.kv_heads + head, scale2, j0, lim, len, li, kc);
   }
   __syncthreads();
   // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
