@@ -30,96 +30,147 @@ struct RopeArgs {
   int64_t tokens;
 };
 
-// A workgroup per TT tokens: first the tokens' cosines and sines, each computed once for all heads,
-// into LDS; then GROUP lanes a head, eight channels a lane.
-template <typename T, int GROUP, bool HALVES, bool VEC>
-__global__ void __launch_bounds__(256) qk_rope_k(RopeArgs a, int tt) {
+// How a channel's pair lies to it: NEXT: beside it; HALF8: in the other half of its axis, all axes of 16
+// channels or multiples of it, so that eight neighbours have eight neighbours; HALF: anywhere.
+enum Pairs { NEXT, HALF8, HALF };
+
+// Sum over the GROUP lanes of a head, on the vector unit.
+template <int GROUP>
+__device__ __forceinline__ float group_sum(float v) {
+  if (GROUP > 1) v += dpp_f<0xB1>(v);   // quad_perm [1, 0, 3, 2]
+  if (GROUP > 2) v += dpp_f<0x4E>(v);   // quad_perm [2, 3, 0, 1]
+  if (GROUP > 4) v += dpp_f<0x141>(v);  // row_half_mirror
+  if (GROUP > 8) v += dpp_f<0x140>(v);  // row_mirror
+  if (GROUP > 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  return v;
+}
+
+// A workgroup takes tt tokens and `steps` steps of 64 / GROUP heads from blockIdx.y * steps on: first the
+// tokens' cosines and sines, each computed once for all heads, into LDS; then a wave a step, GROUP lanes
+// a head, eight channels a lane.  A wave's token is uniform: its addresses are scalar arithmetic.
+template <typename T, int GROUP, Pairs P, bool VEC>
+__global__ void __launch_bounds__(256) qk_rope_k(RopeArgs a, int tt, int steps) {
+  constexpr int HPW = 64 / GROUP;  // heads of a step
   extern __shared__ __align__(16) char lds[];
-  float2* cs = (float2*)lds;                             // [tt][rot / 2]
-  float* rows = (float*)(cs + (int64_t)tt * (a.rot / 2));  // halves: [256][8] normed values
-  const int tid = threadIdx.x, pairs = a.rot / 2, heads = a.q_heads + a.k_heads;
+  const int tid = threadIdx.x, pairs = a.rot / 2, pitch = (pairs + 3) & ~3;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int heads = a.q_heads + a.k_heads, dh = a.dh;
+  float2* cs = (float2*)lds;                             // [tt][pitch]
+  float* mine = (float*)(cs + tt * pitch) + wave * 512;  // HALF8, HALF: 64 lanes' channels
   const int64_t first = (int64_t)blockIdx.x * tt;
   const int n = (int)std::min<int64_t>(tt, a.tokens - first);
+  const int64_t row0 = first / a.S;
+  const int s0 = (int)(first - row0 * a.S);
   for (int i = tid; i < n * pairs; i += 256) {
-    const int64_t tok = first + i / pairs, row = tok / a.S, s = tok - row * a.S;
-    const int p = i % pairs;
+    const int t = i / pairs, p = i - t * pairs;
+    int s = s0 + t;  // below 2^31 + 16
+    int64_t row = row0;
+    if ((unsigned)s >= (unsigned)a.S) row += (unsigned)s / (unsigned)a.S, s = (unsigned)s % (unsigned)a.S;
     int axis = 0, end = a.axis[0] / 2;
     while (p >= end) end += a.axis[++axis] / 2;
     const double turns = (double)a.pos[row * a.pos_row + s * a.ldpos + axis] * a.freqs[p] *
                          0.15915494309189533577;
     float sn, c;
     sincospif(2.f * (float)(turns - floor(turns)), &sn, &c);
-    cs[i] = make_float2(c, sn);
+    cs[t * pitch + p] = make_float2(c, sn);
   }
-  __syncthreads();
-  const int g = tid % GROUP, c0 = g * 8, dh = a.dh;
+  const int g = lane % GROUP, c0 = g * 8;
   const bool in = c0 < dh;
-  // halves: where a channel's pair is, for the eight channels of this lane
-  int pair[8], mate[8];
-  if (HALVES) {
+  float wq[8], wk[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      int at = 0, axis = 0;
-      pair[j] = -1, mate[j] = 0;
-      if (c0 + j < a.rot) {
-        while (c0 + j >= at + a.axis[axis]) at += a.axis[axis++];
-        const int l = c0 + j - at, h = a.axis[axis] / 2;
-        pair[j] = at / 2 + (l < h ? l : l - h);
-        mate[j] = l < h ? h : -h;
-      }
+  for (int j = 0; j < 8; ++j) {
+    wq[j] = a.qw && in ? a.qw[c0 + j] : 1.f;
+    wk[j] = a.kw && in ? a.kw[c0 + j] : 1.f;
+  }
+  // where the pairs of this lane's channels are: their index, and how far the other channel is
+  constexpr int NP = P == HALF ? 8 : 1;
+  int pair[NP], mate[NP];
+#pragma unroll
+  for (int j = 0; j < NP; ++j) {
+    int at = 0, axis = 0;
+    pair[j] = -1, mate[j] = 0;
+    if (c0 + j >= a.rot) continue;
+    if (P == NEXT) {
+      pair[j] = c0 / 2;
+    } else {
+      while (c0 + j >= at + a.axis[axis]) at += a.axis[axis++];
+      const int l = c0 + j - at, h = a.axis[axis] / 2;
+      pair[j] = at / 2 + (l < h ? l : l - h);
+      mate[j] = l < h ? h : -h;
     }
   }
-  for (int u = tid / GROUP; u < n * heads; u += 256 / GROUP) {
-    const int t = u / heads, hd = u - t * heads;
-    const int64_t tok = first + t, row = tok / a.S, s = tok - row * a.S;
-    const bool is_k = hd >= a.q_heads;
-    const int h = is_k ? hd - a.q_heads : hd;
-    const T* src = (const T*)(is_k ? a.k : a.q) + row * (is_k ? a.k_row : a.q_row) +
-                   s * (is_k ? a.ldk : a.ldq) + (int64_t)h * dh;
-    T* dst = (T*)(is_k ? a.ko : a.qo) + row * (is_k ? a.ko_row : a.qo_row) +
-             s * (is_k ? a.ldko : a.ldqo) + (int64_t)h * dh;
-    float x[8];
-    load8<VEC>(src, c0, dh, x);
+  __syncthreads();
+  const int step0 = blockIdx.y * steps;
+  const int ns = std::min(steps, (heads + HPW - 1) / HPW - step0);
+  int t = 0, st = wave, s = s0;
+  int64_t row = row0;
+  while (true) {
+    while (st >= ns) {  // uniform
+      st -= ns, ++t;
+      if (++s == a.S) s = 0, ++row;
+    }
+    if (t >= n) break;
+    const int hd = (step0 + st) * HPW + lane / GROUP;
+    const bool is_k = hd >= a.q_heads, on = in && hd < heads;
+    const int64_t at = (int64_t)(is_k ? hd - a.q_heads : hd) * dh;
+    const T* src = (is_k ? (const T*)a.k + (row * a.k_row + s * a.ldk)
+                         : (const T*)a.q + (row * a.q_row + s * a.ldq)) + at;
+    T* dst = (is_k ? (T*)a.ko + (row * a.ko_row + s * a.ldko)
+                   : (T*)a.qo + (row * a.qo_row + s * a.ldqo)) + at;
+    float x[8], y[8];
+    load8<VEC>(src, c0, on ? dh : 0, x);
     if (a.norm) {
       float sq = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) sq += x[j] * x[j];
+      const float f = rsqrtf(group_sum<GROUP>(sq) / (float)dh + a.eps);
 #pragma unroll
-      for (int m = 1; m < GROUP; m *= 2) sq += __shfl_xor(sq, m);
-      const float f = 1.f / sqrtf(sq / (float)dh + a.eps);
-      const float* w = is_k ? a.kw : a.qw;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = x[j] * f * (w && in ? w[c0 + j] : 1.f);
+      for (int j = 0; j < 8; ++j) x[j] = x[j] * f * (is_k ? wk[j] : wq[j]);
     }
-    float y[8];
-    const float2* c = cs + t * pairs;
-    if (HALVES) {
-      float* mine = rows + (tid - g) * 8;  // this head's channels
+    const float2* c = cs + t * pitch;
+    if constexpr (P == NEXT) {
+      float4 r[2];  // of four pairs: cosine, sine, cosine, sine
+      r[0] = *(const float4*)(c + std::max(pair[0], 0)), r[1] = *(const float4*)(c + std::max(pair[0], 0) + 2);
+      const float co[4] = {r[0].x, r[0].z, r[1].x, r[1].z}, si[4] = {r[0].y, r[0].w, r[1].y, r[1].w};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mine[c0 + j] = x[j];
+      for (int j = 0; j < 4; ++j) {
+        const bool turns = c0 + 2 * j < a.rot;
+        const float u = x[2 * j], v = x[2 * j + 1];
+        y[2 * j] = turns ? u * co[j] - v * si[j] : u;
+        y[2 * j + 1] = turns ? v * co[j] + u * si[j] : v;
+      }
+    } else {
+      float* own = mine + lane * 8;
+      *(float4*)own = make_float4(x[0], x[1], x[2], x[3]);
+      *(float4*)(own + 4) = make_float4(x[4], x[5], x[6], x[7]);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // read by lanes of the same wave
+      if constexpr (P == HALF8) {
+        float o[8], co[8], si[8];
+        const float2* cp = c + std::max(pair[0], 0);
+        *(float4*)o = *(const float4*)(own + mate[0]), *(float4*)(o + 4) = *(const float4*)(own + mate[0] + 4);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        y[j] = x[j];
-        if (pair[j] >= 0) {
-          const float2 r = c[pair[j]];
-          const float o = mine[c0 + j + mate[j]];
-          y[j] = x[j] * r.x + (mate[j] > 0 ? -o : o) * r.y;
+        for (int j = 0; j < 8; j += 2) {
+          const float4 r = *(const float4*)(cp + j);
+          co[j] = r.x, si[j] = r.y, co[j + 1] = r.z, si[j + 1] = r.w;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          y[j] = pair[0] < 0 ? x[j] : x[j] * co[j] + (mate[0] > 0 ? -o[j] : o[j]) * si[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 r = c[std::max(pair[j], 0)];
+          const float o = own[j + mate[j]];
+          y[j] = pair[j] < 0 ? x[j] : x[j] * r.x + (mate[j] > 0 ? -o : o) * r.y;
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; j += 2) {
-        y[j] = x[j], y[j + 1] = x[j + 1];
-        if (c0 + j < a.rot) {
-          const float2 r = c[(c0 + j) / 2];
-          y[j] = x[j] * r.x - x[j + 1] * r.y;
-          y[j + 1] = x[j + 1] * r.x + x[j] * r.y;
-        }
-      }
     }
-    if (in) store8<VEC>(dst, c0, dh, y);
+    if (on) store8<VEC>(dst, c0, dh, y);
+    st += 4;
   }
 }
 
@@ -178,12 +229,18 @@ extern "C" int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_strid
   a.norm = norm, a.eps = eps, a.tokens = (int64_t)rows * S;
   int group = 1;
   while (group * 8 < dh) group *= 2;
-  const int tt = (int)std::max<int64_t>(1, std::min<int64_t>(16, 1024 / (heads * group)));
+  // Few tokens: a step a wave, as many workgroups as that takes; many: about ten steps a wave, which pay
+  // for the tokens' angles and the workgroup's start.
+  const int64_t all = ceil_div(heads, 64 / group);
+  const bool few = a.tokens * all <= 4 * 2048;
+  const int tt = few ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, 40 / all));
+  const int steps = few ? 4 : (int)all;
   const int64_t wgs = ceil_div(a.tokens, tt);
   if (wgs > 8388607) {
     set_error("more tokens than a grid holds");
     return NV_ERR_UNSUPPORTED;
   }
+  const dim3 grid((unsigned)wgs, (unsigned)ceil_div(all, steps));
   auto ok = [](const void* p, int64_t ld, int64_t row) {
     return !p || (aligned16(p) && (ld | row) % 8 == 0);
   };
@@ -191,15 +248,19 @@ extern "C" int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_strid
                    ok(q_heads ? q_out : nullptr, ldqo, qo_row_stride) &&
                    ok(k_heads ? k : nullptr, ldk, k_row_stride) &&
                    ok(k_heads ? k_out : nullptr, ldko, ko_row_stride);
-  const size_t lds = (size_t)tt * (a.rot / 2) * 8 + (halves ? 8192 : 0);
+  // channels without a pair look at the first ones
+  const size_t lds = (size_t)tt * ((a.rot / 2 + 3) & ~3) * 8 + 32 + (halves ? 8192 : 0);
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), lds, (hipStream_t)stream, a, tt);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), lds, (hipStream_t)stream, a, tt, steps);
   };
+  bool by16 = true;
+  for (int i = 0; i < n_axes; ++i) by16 &= axes[i] % 16 == 0;
   auto pick = [&](auto t, auto g) {
     typedef decltype(t) T;
     constexpr int G = decltype(g)::value;
-    if (halves) vec ? go(qk_rope_k<T, G, true, true>) : go(qk_rope_k<T, G, true, false>);
-    else vec ? go(qk_rope_k<T, G, false, true>) : go(qk_rope_k<T, G, false, false>);
+    if (!halves) vec ? go(qk_rope_k<T, G, NEXT, true>) : go(qk_rope_k<T, G, NEXT, false>);
+    else if (by16) vec ? go(qk_rope_k<T, G, HALF8, true>) : go(qk_rope_k<T, G, HALF8, false>);
+    else vec ? go(qk_rope_k<T, G, HALF, true>) : go(qk_rope_k<T, G, HALF, false>);
   };
   auto sized = [&](auto t) {
     switch (group) {
