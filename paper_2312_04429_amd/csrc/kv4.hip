@@ -34,15 +34,16 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int64_t row, int t, i
 
 // ------------------------------------------------------------------------------------ append
 
-// Four lanes a block of 32 channels, eight channels each.
+// Four lanes a block of 32 channels, eight channels each; a head's tokens one after another, as a page has
+// them, so that a workgroup writes whole lines.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
   const bool is_v = blockIdx.z;
   const int64_t row = blockIdx.y;
-  const uint32_t nb = blocks_of(a.dh), lanes = a.heads * nb * 4;  // of a token
-  const uint32_t id = blockIdx.x * 256u + threadIdx.x, t = id / lanes;  // below 2^32: checked
-  const uint32_t u = id - t * lanes, head = u / (nb * 4), c = (u - head * nb * 4) * 8;
-  const int64_t at = t < (uint32_t)a.T ? place_of(a, row, (int)t, head) : -1;
+  const uint32_t nb = blocks_of(a.dh), lanes = nb * 4;  // of a token's head
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x, u = id / lanes;  // below 2^32: checked
+  const uint32_t head = u / (uint32_t)a.T, t = u - head * a.T, c = (id - u * lanes) * 8;
+  const int64_t at = head < (uint32_t)a.heads ? place_of(a, row, (int)t, head) : -1;
   const bool on = at >= 0 && c < (uint32_t)a.dh;
   float x[8];
   const T* src = (const T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) +
@@ -67,10 +68,10 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv4_read_k(Kv4ReadArgs a) {
   const bool is_v = blockIdx.z;
   const int64_t row = blockIdx.y;
-  const uint32_t nb = blocks_of(a.dh), nch = a.dh / 8, lanes = a.heads * nch;
-  const uint32_t id = blockIdx.x * 256u + threadIdx.x, t = id / lanes;  // below 2^32: checked
-  if (t >= (uint32_t)a.T) return;
-  const uint32_t u = id - t * lanes, head = u / nch, c = (u - head * nch) * 8;
+  const uint32_t nb = blocks_of(a.dh), nch = a.dh / 8;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x, u = id / nch;  // below 2^32: checked
+  const uint32_t head = u / (uint32_t)a.T, t = u - head * a.T, c = (id - u * nch) * 8;
+  if (head >= (uint32_t)a.heads) return;
   const int64_t at = place_of(a, row, (int)t, head);
   float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (at >= 0) {
