@@ -38,27 +38,28 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int64_t row, int t, i
 // them, so that a workgroup writes whole lines.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
-  const bool is_v = blockIdx.z;
   const int64_t row = blockIdx.y;
   const uint32_t nb = blocks_of(a.dh), lanes = nb * 4;  // of a token's head
   const uint32_t id = blockIdx.x * 256u + threadIdx.x, u = id / lanes;  // below 2^32: checked
   const uint32_t head = u / (uint32_t)a.T, t = u - head * a.T, c = (id - u * lanes) * 8;
   const int64_t at = head < (uint32_t)a.heads ? place_of(a, row, (int)t, head) : -1;
   const bool on = at >= 0 && c < (uint32_t)a.dh;
-  float x[8];
-  const T* src = (const T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) +
-                 t * (is_v ? a.ldv : a.ldk) + (int64_t)head * a.dh;
-  load8<VEC>(src, c, on ? a.dh : 0, x);
-  float top = 0.f;
+  float x[2][8];
+  load8<VEC>((const T*)a.k + row * a.k_row + t * a.ldk + (int64_t)head * a.dh, c, on ? a.dh : 0, x[0]);
+  load8<VEC>((const T*)a.v + row * a.v_row + t * a.ldv + (int64_t)head * a.dh, c, on ? a.dh : 0, x[1]);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) top = fmaxf(top, abs_or_inf(x[j]));
-  top = fmaxf(top, dpp_f<0xB1>(top));  // quad_perm [1, 0, 3, 2]
-  top = fmaxf(top, dpp_f<0x4E>(top));  // quad_perm [2, 3, 0, 1]
-  if (!on) return;
-  const int e = scale_byte4(top);
-  *(uint32_t*)((is_v ? a.vp : a.kp) + at * (a.dh / 2) + c / 2) =
-      e == 255 ? 0u : codes4x8(x, scale_inverse(e));
-  if (c % KV4_BLOCK == 0) (is_v ? a.vs : a.ks)[at * nb + c / KV4_BLOCK] = (uint8_t)e;
+  for (int i = 0; i < 2; ++i) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, abs_or_inf(x[i][j]));
+    top = fmaxf(top, dpp_f<0xB1>(top));  // quad_perm [1, 0, 3, 2]
+    top = fmaxf(top, dpp_f<0x4E>(top));  // quad_perm [2, 3, 0, 1]
+    if (!on) continue;
+    const int e = scale_byte4(top);
+    *(uint32_t*)((i ? a.vp : a.kp) + at * (a.dh / 2) + c / 2) =
+        e == 255 ? 0u : codes4x8(x[i], scale_inverse(e));
+    if (c % KV4_BLOCK == 0) (i ? a.vs : a.ks)[at * nb + c / KV4_BLOCK] = (uint8_t)e;
+  }
 }
 
 // -------------------------------------------------------------------------------------- read
@@ -66,24 +67,28 @@ __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
 // Eight channels a lane.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv4_read_k(Kv4ReadArgs a) {
-  const bool is_v = blockIdx.z;
   const int64_t row = blockIdx.y;
   const uint32_t nb = blocks_of(a.dh), nch = a.dh / 8;
   const uint32_t id = blockIdx.x * 256u + threadIdx.x, u = id / nch;  // below 2^32: checked
   const uint32_t head = u / (uint32_t)a.T, t = u - head * a.T, c = (id - u * nch) * 8;
   if (head >= (uint32_t)a.heads) return;
   const int64_t at = place_of(a, row, (int)t, head);
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  uint32_t w[2] = {0, 0};
+  int e[2] = {127, 127};
   if (at >= 0) {
-    const uint32_t w = *(const uint32_t*)((is_v ? a.vp : a.kp) + at * (a.dh / 2) + c / 2);
-    const float s = scale_value((is_v ? a.vs : a.ks)[at * nb + c / KV4_BLOCK]);
-    const half8 v = Half8<_Float16>::of(w, 1.f);
+    w[0] = *(const uint32_t*)(a.kp + at * (a.dh / 2) + c / 2), e[0] = a.ks[at * nb + c / KV4_BLOCK];
+    w[1] = *(const uint32_t*)(a.vp + at * (a.dh / 2) + c / 2), e[1] = a.vs[at * nb + c / KV4_BLOCK];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float x[8];
+    const float s = scale_value(e[i]);
+    const half8 v = Half8<_Float16>::of(w[i], 1.f);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = (float)v[j] * s;
+    T* to = i ? (T*)a.v + row * a.v_row + t * a.ldv : (T*)a.k + row * a.k_row + t * a.ldk;
+    store8<VEC>(to + (int64_t)head * a.dh, c, a.dh, x);
   }
-  T* to = (T*)(is_v ? a.v : a.k) + row * (is_v ? a.v_row : a.k_row) + t * (is_v ? a.ldv : a.ldk) +
-          (int64_t)head * a.dh;
-  store8<VEC>(to, c, a.dh, x);
 }
 
 // --------------------------------------------------------------------------------- attention
@@ -941,7 +946,7 @@ extern "C" int32_t nv_op_kv4_append(const void* k, int64_t ldk, int64_t k_row_st
                         ldk, k_row_stride, ldv, v_row_stride, n_pages, table, pos, count,
                         T, heads, dh, table_w};
   const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
-  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows, 2);
+  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
   };
@@ -971,7 +976,7 @@ extern "C" int32_t nv_op_kv4_read(const void* kp, const void* vp, const uint8_t*
   const Kv4ReadArgs a{(const uint8_t*)kp, (const uint8_t*)vp, ks, vs, n_pages, table, pos, count,
                       k, v, ldk, k_row_stride, ldv, v_row_stride, T, heads, dh, table_w};
   const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
-  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows, 2);
+  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
   };
