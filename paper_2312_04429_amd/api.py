@@ -723,9 +723,10 @@ def _pages(pages, dev):
 
 def _strides3(t, what):
     """(token stride, row stride) of t [rows][tokens][columns] with contiguous columns."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    s = t.stride()
+    if len(s) != 3 or (s[2] != 1 and t.shape[2] > 1):
         raise ValueError(f"{what}: [rows][tokens][heads * dh] with contiguous columns expected")
-    return t.stride(1), t.stride(0)
+    return s[1], s[0]
 
 
 def _table(table, rows, dev):
@@ -780,7 +781,7 @@ def _attention(q, cache, table, lens, scale, qpos, out, ws, name):
     if qpos is not None:
         _want(qpos, "qpos", _I32, dev, (rows,), True)
     if out is None:
-        out, ldo, orow = torch.empty((rows, S, cols), dtype=q.dtype, device=q.device), cols, S * cols
+        out, ldo, orow = q.new_empty((rows, S, cols)), cols, S * cols
     else:
         _want(out, "out", (q.dtype,), dev, (rows, S, cols))
         ldo, orow = _strides3(out, "out")
@@ -821,38 +822,42 @@ def nv_op_qk_rope(q, k, dh, pos, axes, freqs, q_weight=None, k_weight=None, eps=
     dev, (ldq, qr) = _dev(q, "q"), _strides3(q, "q")
     _want(q, "q", _HALF, dev)
     rows, S, cols = q.shape
-    if dh < 1 or cols % dh or (k is not None and (k.dim() != 3 or k.shape[2] % dh)):
-        raise ValueError(f"q and k need a multiple of dh = {dh} columns")
-    if len(axes) and (pos.dim() != 3 or (len(axes) > 1 and pos.stride(2) != 1)):
-        raise ValueError("pos: [rows][S][axes] with contiguous axes expected")
-    _want(pos, "pos", _I32, dev, (rows, S, len(axes)))
-    _want(freqs, "freqs", _F64, dev, (sum(axes) // 2,), True)
-    ldk = kr = kh = 0
+    n, ldk, kr, kcols = len(axes), 0, 0, 0
     if k is not None:
-        _want(k, "k", (q.dtype,), dev, (rows, S, k.shape[2]))
-        (ldk, kr), kh = _strides3(k, "k"), k.shape[2] // dh
+        ldk, kr = _strides3(k, "k")
+        kcols = k.shape[2]
+        _want(k, "k", (q.dtype,), dev, (rows, S, kcols))
+    if dh < 1 or cols % dh or kcols % dh:
+        raise ValueError(f"q and k need a multiple of dh = {dh} columns")
+    _want(pos, "pos", _I32, dev, (rows, S, n))
+    ps = pos.stride()
+    if n > 1 and ps[2] != 1:
+        raise ValueError("pos: [rows][S][axes] with contiguous axes expected")
+    _want(freqs, "freqs", _F64, dev, (sum(axes) // 2,), True)
     if eps is None and not (q_weight is None and k_weight is None):
         raise ValueError("weights without a norm (eps is None)")
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _want(w, what, _F32, dev, (dh,), True)
+    if q_weight is not None:
+        _want(q_weight, "q_weight", _F32, dev, (dh,), True)
+    if k_weight is not None:
+        _want(k_weight, "k_weight", _F32, dev, (dh,), True)
+    ldqo, qor, ldko, kor = cols, S * cols, kcols, S * kcols
     if out is None:
-        out = (torch.empty((rows, S, cols), dtype=q.dtype, device=q.device),
-               None if k is None else torch.empty((rows, S, kh * dh), dtype=q.dtype, device=q.device))
-    qo, ko = out
-    _want(qo, "out[0]", (q.dtype,), dev, (rows, S, cols))
-    (ldqo, qor), ldko, kor = _strides3(qo, "out[0]"), 0, 0
-    if k is not None:
-        _want(ko, "out[1]", (q.dtype,), dev, (rows, S, kh * dh))
-        ldko, kor = _strides3(ko, "out[1]")
+        qo, ko = q.new_empty((rows, S, cols)), None if k is None else q.new_empty((rows, S, kcols))
+    else:
+        qo, ko = out
+        _want(qo, "out[0]", (q.dtype,), dev, (rows, S, cols))
+        ldqo, qor = _strides3(qo, "out[0]")
+        if k is not None:
+            _want(ko, "out[1]", (q.dtype,), dev, (rows, S, kcols))
+            ldko, kor = _strides3(ko, "out[1]")
     if S < 2:  # strides of dimensions of one are free; any that the kernel takes will do
-        ldq, ldk, ldqo, ldko = cols, kh * dh, cols, kh * dh
+        ldq, ldk, ldqo, ldko = cols, kcols, cols, kcols
     if rows < 2:
         qr = kr = qor = kor = 0
     _call("nv_op_qk_rope", dev, q.data_ptr(), ldq, qr, qo.data_ptr(), ldqo, qor, cols // dh,
-          _at(q_weight), _at(k), ldk, kr, _at(ko) if kh else None, ldko, kor, kh, _at(k_weight),
-          _DT[q.dtype], rows, S, dh, pos.data_ptr(), pos.stride(1), pos.stride(0), len(axes),
-          (C.c_int32 * len(axes))(*axes), freqs.data_ptr(), halves, eps is not None,
+          _at(q_weight), _at(k), ldk, kr, _at(ko), ldko, kor, kcols // dh, _at(k_weight),
+          _DT[q.dtype], rows, S, dh, pos.data_ptr(), ps[1], ps[0], n,
+          (C.c_int32 * n)(*axes), freqs.data_ptr(), halves, eps is not None,
           0.0 if eps is None else eps)
     return qo, ko
 
@@ -913,14 +918,18 @@ def nv_op_kv4_read(pages, table, pos, T, count=None, dtype=torch.float16, out=No
         _want(count, "count", _I32, dev, (rows,), True)
     if dtype not in _DT:
         raise ValueError("dtype must be float32, float16 or bfloat16")
+    cols = H * dh
     if out is None:
-        out = tuple(torch.empty((rows, T, H * dh), dtype=dtype, device=kp.device) for _ in "kv")
-    k, v = out
-    _want(k, "out[0]", (dtype,), dev, (rows, T, H * dh))
-    _want(v, "out[1]", (dtype,), dev, (rows, T, H * dh))
-    (ldk, kr), (ldv, vr) = _strides3(k, "out[0]"), _strides3(v, "out[1]")
-    if T < 2:
-        ldk = ldv = H * dh
+        k, v = torch.empty((2, rows, T, cols), dtype=dtype, device=kp.device).unbind()
+        ldk = ldv = cols
+        kr = vr = T * cols
+    else:
+        k, v = out
+        _want(k, "out[0]", (dtype,), dev, (rows, T, cols))
+        _want(v, "out[1]", (dtype,), dev, (rows, T, cols))
+        (ldk, kr), (ldv, vr) = _strides3(k, "out[0]"), _strides3(v, "out[1]")
+        if T < 2:
+            ldk = ldv = cols
     _call("nv_op_kv4_read", dev, kp.data_ptr(), vp.data_ptr(), ks.data_ptr(), vs.data_ptr(), n,
           table.data_ptr(), W, pos.data_ptr(), _at(count), rows, T, H, dh, k.data_ptr(), ldk, kr,
           v.data_ptr(), ldv, vr, _DT[dtype])
