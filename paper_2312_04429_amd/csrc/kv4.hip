@@ -97,12 +97,16 @@ __global__ void __launch_bounds__(256) kv4_read_k(Kv4ReadArgs a) {
 // lane's own; accumulators of two 16-token tiles are then the second product's operand as they stand,
 // against values of the same tokens.
 
-// Head dimension in 32-wide steps; lane group kc takes the 8 STEPS channels from 8 STEPS kc on, so
-// that its codes of a token are neighbours.
+// Head dimension in 32-wide steps, of which lane group kc takes eight channels.  NEAR: those of all steps
+// are neighbours (its codes of a token are one load); otherwise a step's 32 are (16-byte units in LDS that
+// groups of lanes read at once lie in different banks).
 template <int DH>
 struct Dims {
   static constexpr int STEPS = (DH + 31) / 32, NB = blocks_of(DH), DV = (DH + 15) / 16;
-  static __device__ __forceinline__ int dim(int step, int kc) { return kc * 8 * STEPS + step * 8; }
+  template <bool NEAR = true>
+  static __device__ __forceinline__ int dim(int step, int kc) {
+    return NEAR ? kc * 8 * STEPS + step * 8 : step * 32 + kc * 8;
+  }
 };
 
 // Pages p0 .. p1 - 1 of share `split` of a tile's pages: equal parts of at least KV8_SHARE pages, so a
@@ -142,7 +146,7 @@ __device__ __forceinline__ void split_bf16(float x, __bf16* hi, __bf16* lo) {
 // every scale; float16 queries, and probabilities, as sums of two.  Everything comes from global memory
 // as it is needed.  j0: the page's first token; lim: tokens this lane's query sees; len: tokens of
 // the sequence.  A NaN block of values reaches the queries that see its token, in its 32 channels.
-template <typename T, int DH>
+template <typename T, int DH, bool NEAR>
 __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>::Vec* fq,
                                          const Kv4AttnArgs& a, int64_t ph, float scale2, int j0,
                                          int lim, int len, int li, int kc) {
@@ -159,7 +163,7 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
     const int tok = 16 * t + li;
 #pragma unroll
     for (int b = 0; b < D::STEPS; ++b) {
-      const int d = D::dim(b, kc);
+      const int d = D::template dim<NEAR>(b, kc);
       bf16x8 k = {}, qh, ql;
       auto fb = fq[b];
       asm volatile("" : "+v"(fb));
@@ -270,11 +274,10 @@ __device__ __forceinline__ bool exact(int e) {
 }
 template <typename T, int DH>
 __device__ __forceinline__ bool exact(int e, const typename Units<DH>::Codes& c) {
-  if (exact<T>(e)) return true;
   uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < Units<DH>::CW / 8; ++i) any |= c.w[i];
-  return e != 255 && (any & 0x77777777u) == 0;
+  return exact<T>(e) | ((e != 255) & ((any & 0x77777777u) == 0));
 }
 __device__ __forceinline__ float scale_bits(int e) { return __int_as_float(e << 23); }
 
@@ -541,7 +544,7 @@ __global__ void __launch_bounds__(256) attn_kv4_k(Kv4AttnArgs a) {
     pc.load_values(a, page * a.kv_heads + head, lane);
     pc.cut(len - j0, lane, li);
     if (!pc.template exact16<T>())
-      page_any<T, DH>(st, fq, a, page * a.kv_heads + head, scale2, j0, lim, len, li, kc);
+      page_any<T, DH, true>(st, fq, a, page * a.kv_heads + head, scale2, j0, lim, len, li, kc);
   }
   __syncthreads();
   // The waves' states, in wave order: means, which are no larger than the values, and their weights (a
@@ -594,10 +597,10 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
   using U = Units<DH>;
   constexpr int NT = NW * 64, COLS = NW * QB * 16;
   constexpr int UPL = (2 * U::N + NT - 1) / NT;  // units of keys, then of values, a lane
-  constexpr int KROW = D::STEPS * 32 + 8, VSIZE = PAGE * Values<DH>::ROW;
+  constexpr int KROW = D::STEPS * 32 + 16, VSIZE = PAGE * Values<DH>::ROW;
   __shared__ __align__(16) T sk[2][PAGE * KROW];
   __shared__ __align__(16) _Float16 sv[2][VSIZE];
-  __shared__ int waits[2];  // page + 1 of the page in a buffer if it waits
+  __shared__ int waits[4];  // [n & 3]: n + 1 if the n-th page waits
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, kc = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rh = blockIdx.x % (a.rows * a.kv_heads);  // a multiple of 8: one XCD's L2 for a head
@@ -616,7 +619,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
 
   Vec fq[QB][D::STEPS];
   State<DH> st[QB];
-  floatx4 sum[QB];  // of a lane's query, four times
+  float sum[QB];
   int lim[QB];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
@@ -626,24 +629,24 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
                     (int64_t)(head * group + col % group) * DH;
 #pragma unroll
     for (int b = 0; b < D::STEPS; ++b) {
-      const int d = D::dim(b, kc);
+      const int d = D::template dim<false>(b, kc);
       fq[qb][b] = d < DH ? *(const Vec*)(qrow + d) : Vec{};
     }
-    st[qb].m = -INFINITY, sum[qb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    st[qb].m = -INFINITY, sum[qb] = 0.f;
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) st[qb].acc[j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // The pages in turn, ph < 0: none left.  A page's table entry was read when the one before it was
+  // taken: its address does not wait for memory.
   struct Page { int64_t ph; int p; };
   int pnext, pages;  // the next page of this share, and its end
   share_of((sees(c0 + COLS - 1) + PAGE - 1) / PAGE, split, a.splits, &pnext, &pages);
   const int first = pnext;
-  const int wave_least = sees(c0 + wave * QB * 16), wave_most = sees(c0 + (wave + 1) * QB * 16 - 1);
-  // The next page that is there (p.ph < 0: none left).  Its table entry was read at the last call:
-  // the page's address does not wait for memory.
+  const int wave_least = sees(c0 + wave * QB * 16);
   int entry = pnext < pages ? table[pnext] : 0;
-  auto take = [&](Page& p) {
-    p.ph = -1;
+  auto take = [&] {
+    Page p{-1, 0};
     while (pnext < pages) {
       const int64_t page = __builtin_amdgcn_readfirstlane(entry);
       p.p = pnext++;
@@ -652,115 +655,116 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
       p.ph = page * a.kv_heads + head;
       break;
     }
+    return p;
   };
-  typename U::Codes code[UPL];
-  int sc[UPL];
-  auto fetch = [&](const Page& p) {
+  typename U::Codes code[UPL] = {};
+  int sc[UPL] = {};
+  auto is_value = [&](int i) {  // the same in all lanes of a wave
+    return U::N % NT == 0 ? i * NT >= U::N : __builtin_amdgcn_readfirstlane(i * NT + tid) >= U::N;
+  };
+  auto in_page = [&](int i) { return 2 * U::N % NT == 0 || i * NT + tid < 2 * U::N; };
+  auto fetch = [&](const Page& pk, const Page& pv) {  // a page's keys, another's values
 #pragma unroll
     for (int i = 0; i < UPL; ++i) {
-      const int u = i * NT + tid;
-      if (2 * U::N % NT != 0 && u >= 2 * U::N) break;  // whole waves
-      const bool is_v = u >= U::N;
-      const int n = is_v ? u - U::N : u;
-      code[i] = U::load((is_v ? a.vp : a.kp) + p.ph * PAGE * (DH / 2), n);
-      sc[i] = U::scale((is_v ? a.vs : a.ks) + p.ph * PAGE * D::NB, n);
+      const bool is_v = is_value(i);
+      const int64_t ph = is_v ? pv.ph : pk.ph;
+      if (ph < 0 || !in_page(i)) continue;
+      const int n = i * NT + tid - (is_v ? U::N : 0);
+      code[i] = U::load((is_v ? a.vp : a.kp) + ph * PAGE * (DH / 2), n);
+      sc[i] = U::scale((is_v ? a.vs : a.ks) + ph * PAGE * D::NB, n);
     }
   };
-  auto stash = [&](const Page& p, int buf) {
-    const int n = len - p.p * PAGE;
+  // The i-th unit into LDS, as 16-bit values.  What they do not hold is zeros there, and its page, the
+  // n-th, waits.
+  bool bad_k = false, bad_v = false;
+  auto stash = [&](int i, const Page& pk, const Page& pv, int bk, int bv) {
+    const bool is_v = is_value(i);
+    if (!in_page(i)) return;
+    const int u = i * NT + tid - (is_v ? U::N : 0), tok = u / U::UPT;
+    // what is behind the sequence may be anything
+    const int e = (is_v ? pv.p : pk.p) * PAGE + tok < len ? sc[i] : 127;
+    const bool ok = is_v ? exact<_Float16, DH>(e, code[i]) : exact<T, DH>(e, code[i]);
+    const float f = ok ? scale_bits(e) : 0.f;
+    if (is_v) {
+      bad_v |= !ok;
+      Values<DH>::store(sv[bv], u, code[i], f);
+    } else {
+      bad_k |= !ok;
+      T* to = sk[bk] + tok * KROW + u % U::UPT * U::CW;
 #pragma unroll
-    for (int i = 0; i < UPL; ++i) {
-      const int u = i * NT + tid;
-      if (2 * U::N % NT != 0 && u >= 2 * U::N) break;
-      const bool is_v = u >= U::N;
-      const int w = is_v ? u - U::N : u, tok = w / U::UPT;
-      int e = sc[i];
-      if (n < PAGE && tok >= n) e = 127;  // what is behind the sequence may be anything
-      if (is_v) {
-        if (!exact<_Float16, DH>(e, code[i])) waits[buf] = p.p + 1;
-        Values<DH>::store(sv[buf], w, code[i], scale_bits(e));
-      } else {
-        if (!exact<T, DH>(e, code[i])) waits[buf] = p.p + 1;
-        T* to = sk[buf] + tok * KROW + w % U::UPT * U::CW;
-#pragma unroll
-        for (int k = 0; k < U::CW / 8; ++k) *(Vec*)(to + k * 8) = M::of(code[i].w[k], scale_bits(e));
-      }
+      for (int k = 0; k < U::CW / 8; ++k) *(Vec*)(to + k * 8) = M::of(code[i].w[k], f);
     }
+  };
+  auto stashed = [&](int nk, int nv) {
+    if (bad_k) waits[nk & 3] = nk + 1;
+    if (bad_v) waits[nv & 3] = nv + 1;
+    bad_k = bad_v = false;
+  };
+  auto stash_all = [&](const Page& p, int n) {
+#pragma unroll
+    for (int i = 0; i < UPL; ++i) stash(i, p, p, n, n);
+    stashed(n, n);
   };
 
-  auto attend = [&](int buf, int j0, bool some) {
-    const T* K_ = sk[buf];
-    // Key fragments are requested TG tiles at a time, VG tiles of values before the softmax, whose
-    // arithmetic covers their way.
-    constexpr int TG = DH >= 128 ? 2 : 4, VG = DH >= 128 ? D::DV / 2 : D::DV;
-    floatx4 s[QB][4];
+  // S = Q K^T, 16 keys at a time
+  Vec fk[2][D::STEPS];
+  auto load_keys = [&](int buf, int t) {
 #pragma unroll
-    for (int t0 = 0; t0 < 4; t0 += TG) {
-      Vec fk[TG][D::STEPS];
-#pragma unroll
-      for (int t = 0; t < TG; ++t)
-#pragma unroll
-        for (int b = 0; b < D::STEPS; ++b) {
-          const int d = D::dim(b, kc);  // past dh: the row's first channels against zeros
-          fk[t][b] = *(const Vec*)(K_ + ((t0 + t) * 16 + li) * KROW + (d < DH ? d : 0));
-        }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int t = 0; t < TG; ++t)
-#pragma unroll
-        for (int b = 0; b < D::STEPS; ++b)
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-            s[qb][t0 + t] =
-                M::mul(fk[t][b], fq[qb][b], b ? s[qb][t0 + t] : floatx4{0.f, 0.f, 0.f, 0.f});
+    for (int b = 0; b < D::STEPS; ++b) {
+      const int d = D::template dim<false>(b, kc);  // past dh: the row's first channels against zeros
+      fk[t & 1][b] = *(const Vec*)(sk[buf] + (t * 16 + li) * KROW + (d < DH ? d : 0));
     }
-    half8 fv[VG][2];
-    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto score = [&](floatx4 (&s)[QB][4], int t) {
 #pragma unroll
-    for (int j = 0; j < VG; ++j)
+    for (int b = 0; b < D::STEPS; ++b)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) fv[j][h] = Values<DH>::load(sv[buf], j, h, li, kc);
-    __builtin_amdgcn_sched_barrier(0);
-    // Scores relative to the query's reference.  It moves only when a probability would pass 2^P_TOP,
-    // and then to where the largest is 2^LOW: low enough that few pages move it, high enough for what
-    // is small beside it.
+      for (int qb = 0; qb < QB; ++qb)
+        s[qb][t] = M::mul(fk[t & 1][b], fq[qb][b], b ? s[qb][t] : floatx4{0.f, 0.f, 0.f, 0.f});
+  };
+  // Scores relative to the query's reference, and the largest of a lane's.
+  float top[QB];
+  auto relate = [&](floatx4 (&s)[QB][4], int tile) {
+    const int qb = tile / 4, t = tile % 4;
+    const float base = st[qb].m == -INFINITY ? 0.f : st[qb].m;
+    if (t == 0) top[qb] = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[qb][t][r] = fmaf(s[qb][t][r], scale2, -base);
+      top[qb] = fmaxf(top[qb], s[qb][t][r]);
+    }
+  };
+  bool late = false;  // some page waits
+  // Masks, and the reference.  It moves only when a probability would pass 2^P_TOP, and then to where the
+  // largest is 2^LOW: low enough that few pages move it, high enough for what is small beside it.
+  auto settle = [&](floatx4 (&s)[QB][4], const Page& cur, int n) {
     constexpr float LOW = 9.f;
-    bool grow = false;
+    const int j0 = cur.p * PAGE;
+    const bool wait = __builtin_amdgcn_readfirstlane(waits[n & 3]) == n + 1;
+    late |= wait;
+    if (wait || j0 + PAGE > wave_least) {  // uniform
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const float base = st[qb].m == -INFINITY ? 0.f : st[qb].m;
-      float top = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[qb][t][r] = fmaf(s[qb][t][r], scale2, -base);
-          top = fmaxf(top, s[qb][t][r]);
-        }
-      if (some) {  // uniform
-        const int n = lim[qb] - j0 - 4 * kc;
-        top = -INFINITY;
+      for (int qb = 0; qb < QB; ++qb) {
+        const int sees_of = wait ? 0 : lim[qb] - j0 - 4 * kc;
+        top[qb] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            if (16 * t + r >= n) s[qb][t][r] = -INFINITY;
-            top = fmaxf(top, s[qb][t][r]);
+            if (16 * t + r >= sees_of) s[qb][t][r] = -INFINITY;
+            top[qb] = fmaxf(top[qb], s[qb][t][r]);
           }
       }
-      grow |= !(top <= P_TOP) || st[qb].m == -INFINITY;
     }
+    bool grow = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) grow |= !(top[qb] <= P_TOP) || st[qb].m == -INFINITY;
     if (__ballot(grow)) {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[qb][t][r]);
-        top = rows_max(top);
+        const float most = rows_max(top[qb]);
         const bool fresh = st[qb].m == -INFINITY;
-        const float low = reference(top, LOW);
+        const float low = reference(most, LOW);
         const float move = low == -INFINITY ? 0.f : fresh ? low : fmaxf(low, 0.f);
         const float mnew = fresh ? low : st[qb].m + move;
         const float alpha = fresh ? 0.f : __builtin_amdgcn_exp2f(-move);
@@ -772,53 +776,91 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
         for (int t = 0; t < 4; ++t) s[qb][t] -= move;
       }
     }
-    half8 fp[QB][2];
+  };
+  half8 fp[QB][2];
+  auto probs = [&](const floatx4 (&s)[QB][4], int t) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
+    for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int r = 0; r < 4; ++r)
+        fp[qb][t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[qb][t][r]);
+  };
+  half8 fv[2][2];
+  auto load_values = [&](int buf, int j) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          fp[qb][t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(s[qb][t][r]);
-      sum[qb] = add_probs(fp[qb], sum[qb]);
-    }
+    for (int h = 0; h < 2; ++h) fv[j & 1][h] = Values<DH>::load(sv[buf], j, h, li, kc);
+  };
+  auto add_values = [&](int j) {
 #pragma unroll
-    for (int j = 0; j < D::DV; ++j)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const half8 v = j < VG ? fv[j < VG ? j : 0][h] : Values<DH>::load(sv[buf], j, h, li, kc);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = V::mul(v, fp[qb][h], st[qb].acc[j]);
-      }
+      for (int qb = 0; qb < QB; ++qb) st[qb].acc[j] = V::mul(fv[j & 1][h], fp[qb][h], st[qb].acc[j]);
   };
 
-  bool late = false;  // some page waits
-  Page cur, ahead;
-  if (tid < 2) waits[tid] = 0;
-  __syncthreads();
-  take(cur);
-  if (cur.ph >= 0) {
-    fetch(cur);
-    stash(cur, 0);
-    take(ahead);
-    if (ahead.ph >= 0) fetch(ahead);
-    int buf = 0;
-    while (true) {
-      __syncthreads();  // the page is in LDS; the other buffer is read no more
-      const int j0 = cur.p * PAGE;
-      const bool wait = __builtin_amdgcn_readfirstlane(waits[buf]) == cur.p + 1;
-      late |= wait;
-      if (j0 < wave_most && !wait) attend(buf, j0, j0 + PAGE > wave_least);
-      if (ahead.ph < 0) break;
-      stash(ahead, buf ^ 1);
-      cur = ahead;
-      take(ahead);
-      if (ahead.ph >= 0) fetch(ahead);
-      buf ^= 1;
+  // Page n in step n.  Its keys were multiplied in the step before; in this one its exponentials run
+  // beside the product of page n + 1's keys, whose scores take their place, and the values' product beside
+  // those scores' arithmetic and the conversion of page n + 2's keys and n + 1's values, whose codes came
+  // a step ahead.  Page n's values are in sv[n & 1], page n + 1's keys in sk[n + 1 & 1]; what is written
+  // was read in the step before.  Within a step the order is kept (left to itself the compiler requests
+  // every operand at the start, and spills): the operands of the next 16 keys or channels are on their way
+  // during these products.
+  Page p0 = take();
+  if (tid < 4) waits[tid] = 0;
+  if (p0.ph >= 0) {
+    Page p1 = take(), p2 = take();
+    floatx4 s[QB][4];
+    fetch(p0, p0);
+    __syncthreads();  // waits
+    stash_all(p0, 0);
+    fetch(p1, p1);
+    stash_all(p1, 1);  // page 1's values once more in step 0
+    fetch(p2, p1);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) load_keys(0, t), score(s, t);
+#pragma unroll
+    for (int i = 0; i < QB * 4; ++i) relate(s, i);
+    __syncthreads();
+    int n = 0;
+    while (p1.ph >= 0) {
+      const int now = n & 1;
+      load_keys(now ^ 1, 0);
+      settle(s, p0, n);
+      probs(s, 0);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        if (t < 3) load_keys(now ^ 1, t + 1);
+        else load_values(now, 0);
+        score(s, t);
+        if (t < 3) probs(s, t + 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) sum[qb] += add_probs(fp[qb], floatx4{0.f, 0.f, 0.f, 0.f})[0];
+#pragma unroll
+      for (int j = 0; j < D::DV; ++j) {
+        if (j + 1 < D::DV) load_values(now, j + 1);
+        add_values(j);
+#pragma unroll
+        for (int i = j * QB * 4 / D::DV; i < (j + 1) * QB * 4 / D::DV; ++i) relate(s, i);
+        if (j < UPL) stash(j, p2, p1, now, now ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      stashed(n + 2, n + 1);
+      p0 = p1, p1 = p2, p2 = take(), ++n;
+      fetch(p2, p1);
+      __syncthreads();
     }
+    settle(s, p0, n);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) probs(s, t);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) sum[qb] += add_probs(fp[qb], floatx4{0.f, 0.f, 0.f, 0.f})[0];
+#pragma unroll
+    for (int j = 0; j < D::DV; ++j) load_values(n & 1, j), add_values(j);
   }
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) st[qb].l = sum[qb][0];
+  for (int qb = 0; qb < QB; ++qb) st[qb].l = sum[qb];
   // The pages that wait: the same rule tells which they are.
   for (int p = first; late && p < pages; ++p) {
     const int64_t page = __builtin_amdgcn_readfirstlane(table[p]);
@@ -837,7 +879,7 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
     auto take_in = [&](auto n) {  // (a loop of two would be kept, its state in memory)
       constexpr int qb = decltype(n)::value;
       if (__ballot(lim[qb] > p * PAGE))
-        page_any<T, DH>(st[qb], fq[qb], a, ph, scale2, p * PAGE, lim[qb], len, li, kc);
+        page_any<T, DH, false>(st[qb], fq[qb], a, ph, scale2, p * PAGE, lim[qb], len, li, kc);
     };
     take_in(std::integral_constant<int, 0>());
     if constexpr (QB > 1) take_in(std::integral_constant<int, 1>());
