@@ -605,7 +605,10 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rh = blockIdx.x % (a.rows * a.kv_heads);  // a multiple of 8: one XCD's L2 for a head
   const int rest = blockIdx.x / (a.rows * a.kv_heads), split = rest / a.col_tiles;
-  const int ct = a.col_tiles - 1 - rest % a.col_tiles;
+  // Longest first, where not all are resident at once; where they are, a compute unit's second workgroup
+  // is as short as its first is long (a causal limit from 2048 of 4096 tokens: 126 -> 117 us).
+  const int nth = rest % a.col_tiles, half = (a.col_tiles + 1) / 2;
+  const int ct = nth < half || gridDim.x > 512 ? a.col_tiles - 1 - nth : nth - half;
   const int head = rh % a.kv_heads, row = rh / a.kv_heads;
   const int group = a.heads / a.kv_heads, cols = a.S * group, c0 = ct * COLS;
   const int len = (int)std::min<int64_t>(std::max(a.lens[row], 0), (int64_t)a.table_w * PAGE);

@@ -469,6 +469,32 @@ def test_attention_peaked_and_large_scores(S, G):
 
 
 @pytest.mark.parametrize("S,G", SIZES)
+@pytest.mark.parametrize("dh", [64, 128])
+def test_attention_queries_of_unlike_channels(S, G, dh):
+    """One channel of some queries far above the others, on keys that are zero there and on some that are
+    not; queries of the type's smallest numbers, of one channel alone, of zeros."""
+    for dtype in (F16, BF16):
+        for far in (100.0, 3000.0, 50000.0):
+            pages, table = a_cache(4, 1, 4, 1, dh)
+            values = O.values(pages[0], pages[2])
+            values[..., 5] = np.where(np.arange(64) % 16 == 3, 2.0 ** -10, 0)
+            pages[0], pages[2] = O.quantise(values)
+            q = rand(5, 1, S, G * dh, dtype=dtype)
+            q[0, ::2, 5] = far
+            q[0, 1::3, dh - 1] = 0
+            q[0, 2::5, :32] *= 2.0 ** -12
+            q[0, 3::7, 1:] = 0
+            q[0, 4::7] = torch.finfo(dtype).tiny
+            q[0, 5::7] = 0
+            check_attention(q, pages, table, [256], dh ** -0.5, 1)
+            check_attention(q, pages, table, [250], dh ** -0.5, 1, [250 - S])
+        q[0, S // 2, 7], q[0, 0, 9] = float("inf"), float("nan")
+        out = nv().nv_op_attention_kv4(q, to_pages(pages), i32(table), i32([250]), dh ** -0.5)
+        assert torch.isnan(out[0, S // 2, :dh]).all() and torch.isnan(out[0, 0, :dh]).all()
+        assert torch.isnan(out).sum() == (2 if S > 1 else 1) * dh
+
+
+@pytest.mark.parametrize("S,G", SIZES)
 def test_attention_nan_reaches_only_who_sees_it(S, G):
     """NaN blocks of keys and values before some query's limit and behind another's."""
     for dtype in (F16, BF16):
