@@ -660,42 +660,45 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
     }
     return p;
   };
-  typename U::Codes code[UPL] = {};
-  int sc[UPL] = {};
+  struct Coded {
+    typename U::Codes w;
+    int e;
+  };
+  Coded code[UPL] = {};
   auto is_value = [&](int i) {  // the same in all lanes of a wave
     return U::N % NT == 0 ? i * NT >= U::N : __builtin_amdgcn_readfirstlane(i * NT + tid) >= U::N;
   };
   auto in_page = [&](int i) { return 2 * U::N % NT == 0 || i * NT + tid < 2 * U::N; };
-  auto fetch = [&](const Page& pk, const Page& pv) {  // a page's keys, another's values
+  auto fetch = [&](Coded (&code)[UPL], const Page& pk, const Page& pv) {  // a page's keys, another's values
 #pragma unroll
     for (int i = 0; i < UPL; ++i) {
       const bool is_v = is_value(i);
       const int64_t ph = is_v ? pv.ph : pk.ph;
       if (ph < 0 || !in_page(i)) continue;
       const int n = i * NT + tid - (is_v ? U::N : 0);
-      code[i] = U::load((is_v ? a.vp : a.kp) + ph * PAGE * (DH / 2), n);
-      sc[i] = U::scale((is_v ? a.vs : a.ks) + ph * PAGE * D::NB, n);
+      code[i].w = U::load((is_v ? a.vp : a.kp) + ph * PAGE * (DH / 2), n);
+      code[i].e = U::scale((is_v ? a.vs : a.ks) + ph * PAGE * D::NB, n);
     }
   };
   // The i-th unit into LDS, as 16-bit values.  What they do not hold is zeros there, and its page, the
   // n-th, waits.
   bool bad_k = false, bad_v = false;
-  auto stash = [&](int i, const Page& pk, const Page& pv, int bk, int bv) {
+  auto stash = [&](const Coded& c, int i, const Page& pk, const Page& pv, int bk, int bv) {
     const bool is_v = is_value(i);
     if (!in_page(i)) return;
     const int u = i * NT + tid - (is_v ? U::N : 0), tok = u / U::UPT;
     // what is behind the sequence may be anything
-    const int e = (is_v ? pv.p : pk.p) * PAGE + tok < len ? sc[i] : 127;
-    const bool ok = is_v ? exact<_Float16, DH>(e, code[i]) : exact<T, DH>(e, code[i]);
+    const int e = (is_v ? pv.p : pk.p) * PAGE + tok < len ? c.e : 127;
+    const bool ok = is_v ? exact<_Float16, DH>(e, c.w) : exact<T, DH>(e, c.w);
     const float f = ok ? scale_bits(e) : 0.f;
     if (is_v) {
       bad_v |= !ok;
-      Values<DH>::store(sv[bv], u, code[i], f);
+      Values<DH>::store(sv[bv], u, c.w, f);
     } else {
       bad_k |= !ok;
       T* to = sk[bk] + tok * KROW + u % U::UPT * U::CW;
 #pragma unroll
-      for (int k = 0; k < U::CW / 8; ++k) *(Vec*)(to + k * 8) = M::of(code[i].w[k], f);
+      for (int k = 0; k < U::CW / 8; ++k) *(Vec*)(to + k * 8) = M::of(c.w.w[k], f);
     }
   };
   auto stashed = [&](int nk, int nv) {
@@ -703,9 +706,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
     if (bad_v) waits[nv & 3] = nv + 1;
     bad_k = bad_v = false;
   };
-  auto stash_all = [&](const Page& p, int n) {
+  auto stash_all = [&](const Coded (&code)[UPL], const Page& p, int n) {
 #pragma unroll
-    for (int i = 0; i < UPL; ++i) stash(i, p, p, n, n);
+    for (int i = 0; i < UPL; ++i) stash(code[i], i, p, p, n, n);
     stashed(n, n);
   };
 
@@ -812,12 +815,12 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
   if (p0.ph >= 0) {
     Page p1 = take(), p2 = take();
     floatx4 s[QB][4];
-    fetch(p0, p0);
+    Coded second[UPL] = {};
+    fetch(code, p0, p0), fetch(second, p1, p1);
     __syncthreads();  // waits
-    stash_all(p0, 0);
-    fetch(p1, p1);
-    stash_all(p1, 1);  // page 1's values once more in step 0
-    fetch(p2, p1);
+    stash_all(code, p0, 0);
+    stash_all(second, p1, 1);  // page 1's values once more in step 0
+    fetch(code, p2, p1);
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 4; ++t) load_keys(0, t), score(s, t);
@@ -846,12 +849,12 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
         add_values(j);
 #pragma unroll
         for (int i = j * QB * 4 / D::DV; i < (j + 1) * QB * 4 / D::DV; ++i) relate(s, i);
-        if (j < UPL) stash(j, p2, p1, now, now ^ 1);
+        if (j < UPL) stash(code[j], j, p2, p1, now, now ^ 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       stashed(n + 2, n + 1);
       p0 = p1, p1 = p2, p2 = take(), ++n;
-      fetch(p2, p1);
+      fetch(code, p2, p1);
       __syncthreads();
     }
     settle(s, p0, n);
