@@ -23,6 +23,7 @@ import pytest
 import torch
 
 from oracle import ops4 as O
+from ops4_sizes import PLAN_SIZES
 
 pytestmark = pytest.mark.gpu
 
@@ -311,12 +312,16 @@ def test_read_into_views_and_of_any_byte():
 
 # ----------------------------------------------------------------------------- attention_kv4
 
-def check_attention(q, pages, table, lens, scale, H, qpos=None, **kw):
-    """q device [R][S][Hq * dh]; the rest NumPy."""
+def check_attention(q, pages, table, lens, scale, H, qpos=None, copies=1, **kw):
+    """q device [R][S][Hq * dh]; the rest NumPy.  copies: the rows so many times over."""
     R, S, C = q.shape
     dh = 2 * pages[0].shape[3]
-    out = nv().nv_op_attention_kv4(q, to_pages(pages), i32(table), i32(lens), scale,
-                                   qpos=None if qpos is None else i32(qpos), **kw)
+    many = lambda a: i32(np.concatenate([np.asarray(a)] * copies))
+    out = nv().nv_op_attention_kv4(q.repeat(copies, 1, 1) if copies > 1 else q, to_pages(pages), many(table),
+                                   many(lens), scale, qpos=None if qpos is None else many(qpos), **kw)
+    for i in range(1, copies):
+        assert np.array_equal(bits(out[:R]), bits(out[i * R:(i + 1) * R])), i
+    out = out[:R]
     with np.errstate(invalid="ignore", over="ignore"):
         o, spread, size, most = O.attention(np64(q).reshape(R, S, C // dh, dh), *pages, table, lens,
                                             scale, H, qpos)
@@ -411,9 +416,24 @@ def test_attention_tall():
                         [n - S for n in lens] if causal else None)
 
 
+@pytest.mark.parametrize("tile,shares", sorted(PLAN_SIZES))
+def test_attention_plans(tile, shares):
+    """Every tile of queries with every join of shares: rows of differing length, holes, a causal
+    limit."""
+    for i, (R, S, Hq, H, dh, W) in enumerate(PLAN_SIZES[tile, shares]):
+        print("attention_kv4 plan", R, S, Hq, H, dh, W, flush=True)
+        pages, table = a_cache(S + W, R, W, H, dh)
+        lens = [W * 64 - (W * 23 * r) % (W * 64) for r in range(R)]
+        spoil(pages, table, lens)
+        if i:
+            table[0, W // 2] = -1
+        q = rand(S + W, R, S, Hq * dh, dtype=(BF16, F16)[i])
+        check_attention(q, pages, table, lens, dh ** -0.5, H, [n - S for n in lens] if i else None)
+
+
 def test_attention_holes_and_bad_pages():
     R, H, dh, W = 3, 2, 64, 6
-    for S in (2, 90):
+    for S in (2, 90, 300):
         pages, table = a_cache(1, R, W, H, dh)
         table[0, 1], table[0, 5], table[1, 0], table[2] = -1, 10 ** 6, -7, -1
         q = rand(1, R, S, 4 * dh, dtype=F16)
@@ -424,11 +444,12 @@ def test_attention_holes_and_bad_pages():
         check_attention(q, pages, table, [384, 300, 384], 0.1, H, [2 ** 31 - 1, 200, -2 ** 31])
 
 
-SIZES = [(1, 1), (9, 1), (40, 1), (200, 1), (1, 4), (70, 4)]  # queries, query heads a head
+# Queries, query heads a head, copies of the rows: tiles of 16 queries (the first four), of 64, of 128.
+SIZES = [(1, 1, 1), (9, 1, 1), (1, 4, 1), (40, 1, 1), (300, 1, 1), (70, 4, 1), (120, 4, 96)]
 
 
-@pytest.mark.parametrize("S,G", SIZES)
-def test_attention_scales_far_apart(S, G):
+@pytest.mark.parametrize("S,G,N", SIZES)
+def test_attention_scales_far_apart(S, G, N):
     """Values and keys past what a float16 operand holds, in any order, one token of them or blocks of a
     token; blocks of zeros."""
     for dtype in (F16, BF16):
@@ -452,12 +473,12 @@ def test_attention_scales_far_apart(S, G):
                 for i in (0, 1):
                     pages[i][table[0, 0], :, 40] = 0
                     pages[i + 2][table[0, 0], :, 40] = 1
-                check_attention(q, pages, table, [320], dh ** -0.5, 1)
-                check_attention(q, pages, table, [310], dh ** -0.5, 1, [310 - S])
+                check_attention(q, pages, table, [320], dh ** -0.5, 1, copies=N)
+                check_attention(q, pages, table, [310], dh ** -0.5, 1, [310 - S], copies=N)
 
 
-@pytest.mark.parametrize("S,G", SIZES)
-def test_attention_peaked_and_large_scores(S, G):
+@pytest.mark.parametrize("S,G,N", SIZES)
+def test_attention_peaked_and_large_scores(S, G, N):
     """References that move late, scores of hundreds, one key that takes all."""
     for dtype in (F16, BF16):
         pages, table = a_cache(4, 2, 8, 1, 128)
@@ -465,12 +486,12 @@ def test_attention_peaked_and_large_scores(S, G):
         pages[2][table[1, 7], :, 3] += 9
         q = rand(5, 2, S, G * 128, dtype=dtype)
         for lens, scale in (([512, 512], 0.1), ([512, 449], -0.1), ([512, 449], 0.0)):
-            check_attention(q, pages, table, lens, scale, 1)
+            check_attention(q, pages, table, lens, scale, 1, copies=N)
 
 
-@pytest.mark.parametrize("S,G", SIZES)
+@pytest.mark.parametrize("S,G,N", SIZES)
 @pytest.mark.parametrize("dh", [64, 128])
-def test_attention_queries_of_unlike_channels(S, G, dh):
+def test_attention_queries_of_unlike_channels(S, G, N, dh):
     """One channel of some queries far above the others, on keys that are zero there and on some that are
     not; queries of the type's smallest numbers, of one channel alone, of zeros."""
     for dtype in (F16, BF16):
@@ -486,16 +507,16 @@ def test_attention_queries_of_unlike_channels(S, G, dh):
             q[0, 3::7, 1:] = 0
             q[0, 4::7] = torch.finfo(dtype).tiny
             q[0, 5::7] = 0
-            check_attention(q, pages, table, [256], dh ** -0.5, 1)
-            check_attention(q, pages, table, [250], dh ** -0.5, 1, [250 - S])
+            check_attention(q, pages, table, [256], dh ** -0.5, 1, copies=N)
+            check_attention(q, pages, table, [250], dh ** -0.5, 1, [250 - S], copies=N)
         q[0, S // 2, 7], q[0, 0, 9] = float("inf"), float("nan")
         out = nv().nv_op_attention_kv4(q, to_pages(pages), i32(table), i32([250]), dh ** -0.5)
         assert torch.isnan(out[0, S // 2, :dh]).all() and torch.isnan(out[0, 0, :dh]).all()
         assert torch.isnan(out).sum() == (2 if S > 1 else 1) * dh
 
 
-@pytest.mark.parametrize("S,G", SIZES)
-def test_attention_nan_reaches_only_who_sees_it(S, G):
+@pytest.mark.parametrize("S,G,N", SIZES)
+def test_attention_nan_reaches_only_who_sees_it(S, G, N):
     """NaN blocks of keys and values before some query's limit and behind another's."""
     for dtype in (F16, BF16):
         pages, table = a_cache(6, 1, 4, 1, 64)
@@ -504,20 +525,20 @@ def test_attention_nan_reaches_only_who_sees_it(S, G):
         at = 250 - (S + 1) // 2
         page = table[0, at // 64]
         pages[3][page, 0, at % 64, 1] = 255
-        out = check_attention(q, pages, table, [251], 0.125, 1, [first])
+        out = check_attention(q, pages, table, [251], 0.125, 1, [first], copies=N)
         if S > 1:
             assert torch.isnan(out).any() and not torch.isnan(out[0, :S // 2 - 1]).any()
             assert not torch.isnan(out.view(1, S, G, 64)[..., :32]).any()
         pages[2][page, 0, at % 64, 0] = 255
-        check_attention(q, pages, table, [251], 0.125, 1, [first])
-        check_attention(q, pages, table, [at], 0.125, 1)  # nobody sees it
+        check_attention(q, pages, table, [251], 0.125, 1, [first], copies=N)
+        check_attention(q, pages, table, [at], 0.125, 1, copies=N)  # nobody sees it
         for i in (2, 3):
             pages, table = a_cache(6, 1, 4, 1, 64)
             pages[i][table[0, 3]] = 255
             pages[i][table[0, 0], :, 9] = 255
-            check_attention(q, pages, table, [251], 0.125, 1, [first])
-            check_attention(q, pages, table, [192], 0.125, 1)
-            check_attention(q, pages, table, [192], 0.125, 1, [9 - S])
+            check_attention(q, pages, table, [251], 0.125, 1, [first], copies=N)
+            check_attention(q, pages, table, [192], 0.125, 1, copies=N)
+            check_attention(q, pages, table, [192], 0.125, 1, [9 - S], copies=N)
 
 
 def test_attention_strides():
