@@ -664,14 +664,15 @@ int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_stride, void* q_
  *   int32 [rows]; a negative one stores nothing) of its sequence.  Only their own bytes
  *   change: tokens that are there may be written again, in any order; tokens past the
  *   table's end are dropped.  One place in the cache may be named once in a call.
- *   T * heads * 4 ceil(dh / 32) < 2^32 - 255 (beyond: NV_ERR_UNSUPPORTED).
+ *   T * heads * 4 ceil(dh / 32) <= 2^32 - 512 (beyond: NV_ERR_UNSUPPORTED).
  *
  * nv_op_kv4_read: tokens pos[r] .. pos[r] + count[r] - 1 of each row's sequence as
  *   k and v in dtype (NV_F32, NV_F16, NV_BF16), laid out as for append, rows of T
  *   tokens; what is not held (past count[r] or the table's end, in a hole, pos[r] < 0)
  *   is written as zeros.  float32 and bfloat16 hold every value exactly (but for
  *   infinity from 2^128 on: largest magnitudes above 3.5 * 2^126), float16 rounds and
- *   overflows to infinity.  T * heads * dh / 8 < 2^32 - 255.
+ *   overflows to infinity.  T * heads * dh / 8 <= 2^32 - 512 (beyond:
+ *   NV_ERR_UNSUPPORTED).
  *
  * nv_op_attention_kv4: o[i] = sum_j softmax_j(scale q[i] . k_j) v_j over the
  *   tokens j < lens[r] (device int32 [rows], clamped to the table's tokens) of
@@ -685,8 +686,8 @@ int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_stride, void* q_
  *   keys their whole result, one of values its 32 channels.  float32 scores, softmax
  *   and sums; the probabilities enter the second product rounded to 2^-11 of
  *   themselves or 2^-34 of the query's largest, and the same rounded ones make the
- *   sum it is divided by.  Values of 2^90 and more may overflow the sums, values below
- *   2^-126 may count as zero.  scale finite.
+ *   sum it is divided by.  Values of 2^90 and more may overflow the sums, keys and
+ *   values below 2^-126 may count as zero.  scale finite.
  *   workspace: device, >= nv_op_attention_kv4_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV4_PAGE 64

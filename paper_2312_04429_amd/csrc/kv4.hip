@@ -34,8 +34,10 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int64_t row, int t, i
 
 // ------------------------------------------------------------------------------------ append
 
-// Four lanes a block of 32 channels, eight channels each; a head's tokens one after another, as a page has
-// them, so that a workgroup writes whole lines.
+// Four lanes a block of 32 channels, eight channels of keys and values each; a head's tokens one after
+// another, as a page has them, so that a workgroup writes whole lines.  Bound by launch and latency for single
+// tokens (64 of 8 heads of 128: 3.4 us), by HBM for prompts (11680 tokens of 8 heads of 128, float16: 60 MB
+// in 13.8 us, 4.4 TB/s; with keys and values in workgroups of their own 16.5, with two units a lane 15.1).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
   const int64_t row = blockIdx.y;
@@ -64,30 +66,45 @@ __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
 
 // -------------------------------------------------------------------------------------- read
 
-// Eight channels a lane.
-template <typename T, bool VEC>
+// Units of eight channels from which on a lane takes two at once: their way from a position over the
+// table to the tokens is waited for once.
+constexpr int64_t READ_TWO = 1 << 19;
+
+// Eight channels of a token's keys and values a lane, N times; a token's heads one after another, as the
+// output has them.  Bound by HBM's writes: 8 x 4096 tokens of 8 heads of 128 (134 MB out) 34 us with operands
+// and outputs in turn (one unit a lane: 37 to 39; a head's tokens one after another: 40).
+template <typename T, bool VEC, int N>
 __global__ void __launch_bounds__(256) kv4_read_k(Kv4ReadArgs a) {
   const int64_t row = blockIdx.y;
   const uint32_t nb = blocks_of(a.dh), nch = a.dh / 8;
-  const uint32_t id = blockIdx.x * 256u + threadIdx.x, u = id / nch;  // below 2^32: checked
-  const uint32_t head = u / (uint32_t)a.T, t = u - head * a.T, c = (id - u * nch) * 8;
-  if (head >= (uint32_t)a.heads) return;
-  const int64_t at = place_of(a, row, (int)t, head);
-  uint32_t w[2] = {0, 0};
-  int e[2] = {127, 127};
-  if (at >= 0) {
-    w[0] = *(const uint32_t*)(a.kp + at * (a.dh / 2) + c / 2), e[0] = a.ks[at * nb + c / KV4_BLOCK];
-    w[1] = *(const uint32_t*)(a.vp + at * (a.dh / 2) + c / 2), e[1] = a.vs[at * nb + c / KV4_BLOCK];
+  uint32_t t[N], col[N], w[N][2];
+  int e[N][2];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const uint32_t id = (blockIdx.x * N + n) * 256u + threadIdx.x, u = id / nch;  // below 2^32: checked
+    t[n] = u / (uint32_t)a.heads;
+    const uint32_t head = u - t[n] * a.heads, c = (id - u * nch) * 8;
+    col[n] = head * a.dh + c;
+    const int64_t at = t[n] < (uint32_t)a.T ? place_of(a, row, (int)t[n], head) : -1;
+    w[n][0] = w[n][1] = 0, e[n][0] = e[n][1] = 127;
+    if (at >= 0) {
+      w[n][0] = *(const uint32_t*)(a.kp + at * (a.dh / 2) + c / 2), e[n][0] = a.ks[at * nb + c / KV4_BLOCK];
+      w[n][1] = *(const uint32_t*)(a.vp + at * (a.dh / 2) + c / 2), e[n][1] = a.vs[at * nb + c / KV4_BLOCK];
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float x[8];
-    const float s = scale_value(e[i]);
-    const half8 v = Half8<_Float16>::of(w[i], 1.f);
+  for (int n = 0; n < N; ++n) {
+    if (t[n] >= (uint32_t)a.T) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)v[j] * s;
-    T* to = i ? (T*)a.v + row * a.v_row + t * a.ldv : (T*)a.k + row * a.k_row + t * a.ldk;
-    store8<VEC>(to + (int64_t)head * a.dh, c, a.dh, x);
+    for (int i = 0; i < 2; ++i) {
+      float x[8];
+      const float s = scale_value(e[n][i]);
+      const half8 v = Half8<_Float16>::of(w[n][i], 1.f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = (float)v[j] * s;
+      T* to = i ? (T*)a.v + row * a.v_row + t[n] * a.ldv : (T*)a.k + row * a.k_row + t[n] * a.ldk;
+      store8<VEC>(to, col[n], a.heads * a.dh, x);
+    }
   }
 }
 
@@ -964,7 +981,7 @@ int32_t check_tokens(int32_t dtype, bool f32, int32_t rows, int32_t T, int32_t h
     set_error("dh must be 16, 32, 40, 64, 80, 128 or 160");
     return NV_ERR_UNSUPPORTED;
   }
-  if ((int64_t)T * heads * lanes > 0xFFFFFF00ll) {  // threads of a grid's first dimension
+  if ((int64_t)T * heads * lanes > 0xFFFFFE00ll) {  // threads of a grid's first dimension
     set_error("more tokens of a row than a grid holds");
     return NV_ERR_UNSUPPORTED;
   }
@@ -1024,13 +1041,19 @@ extern "C" int32_t nv_op_kv4_read(const void* kp, const void* vp, const uint8_t*
   const Kv4ReadArgs a{(const uint8_t*)kp, (const uint8_t*)vp, ks, vs, n_pages, table, pos, count,
                       k, v, ldk, k_row_stride, ldv, v_row_stride, T, heads, dh, table_w};
   const bool vec = (ldk | ldv | k_row_stride | v_row_stride) % 8 == 0 && aligned16(k) && aligned16(v);
-  const dim3 grid((unsigned)ceil_div((int64_t)T * heads * lanes, 256), rows);
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, a);
+  const int64_t units = (int64_t)T * heads * lanes;
+  auto go = [&](auto kernel, int n) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(units, 256 * n), rows), dim3(256), 0,
+                       (hipStream_t)stream, a);
   };
-  if (dtype == NV_F32) vec ? go(kv4_read_k<float, true>) : go(kv4_read_k<float, false>);
-  else if (dtype == NV_F16) vec ? go(kv4_read_k<_Float16, true>) : go(kv4_read_k<_Float16, false>);
-  else vec ? go(kv4_read_k<__bf16, true>) : go(kv4_read_k<__bf16, false>);
+  auto pick = [&](auto t) {
+    typedef decltype(t) Ty;
+    if (units * rows < READ_TWO) vec ? go(kv4_read_k<Ty, true, 1>, 1) : go(kv4_read_k<Ty, false, 1>, 1);
+    else vec ? go(kv4_read_k<Ty, true, 2>, 2) : go(kv4_read_k<Ty, false, 2>, 2);
+  };
+  if (dtype == NV_F32) pick(float());
+  else if (dtype == NV_F16) pick(_Float16());
+  else pick(__bf16());
   NV_LAUNCH_CHECK("kv4_read_k");
   return NV_OK;
 }
