@@ -50,7 +50,10 @@ __device__ __forceinline__ float group_sum(float v) {
 
 // A workgroup takes tt tokens and `steps` steps of 64 / GROUP heads from blockIdx.y * steps on: first the
 // tokens' cosines and sines, each computed once for all heads, into LDS; then a wave a step, GROUP lanes
-// a head, eight channels a lane.  A wave's token is uniform: its addresses are scalar arithmetic.
+// a head, eight channels a lane.  A wave's token is uniform: its addresses are scalar arithmetic (with a
+// 64-bit division by S a lane and step, 16384 tokens of 40 heads of 128 took 158 us).  Bound by HBM: those
+// tokens, bfloat16, three axes: 335 MB in 78 us (4.3 TB/s); 8346 tokens of 40 heads of 64, float16: 22 us
+// (3.8); 32 single tokens of 40 heads of 128: 4.9 us, launch and the way from a position to its angles.
 template <typename T, int GROUP, Pairs P, bool VEC>
 __global__ void __launch_bounds__(256) qk_rope_k(RopeArgs a, int tt, int steps) {
   constexpr int HPW = 64 / GROUP;  // heads of a step
