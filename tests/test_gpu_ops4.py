@@ -290,6 +290,45 @@ def test_append_of_what_is_not_finite_and_of_views():
     check_append(one, one, pages, table, np.array([5, 1]), [70, 3], H)
 
 
+def test_tokens_written_in_any_order_and_again():
+    """Parts of a prompt last one first, some of it twice: the cache of one call, nothing else touched."""
+    R, H, dh, T = 2, 2, 80, 150
+    k, v = rand(1, R, T, H * dh, dtype=F16), rand(2, R, T, H * dh, dtype=F16)
+    table = i32([[4, 1, 5], [0, 3, 2]])
+    one, parts = (to_pages(pages_np(3, 7, H, dh)) for _ in range(2))
+    pos = np.array([3, 40])
+    nv().nv_op_kv4_append(k, v, one, table, i32(pos))
+    for a, b in ((100, 150), (7, 101), (0, 70), (20, 21)):
+        nv().nv_op_kv4_append(k[:, a:b], v[:, a:b], parts, table, i32(pos + a))
+    for a, b in zip(one, parts):
+        assert torch.equal(a, b)
+
+
+def test_cache_past_32_bits():
+    """Pages whose codes lie more than 2^32 bytes into the cache: written, read and attended as the same
+    pages of a small cache."""
+    H, dh, n = 8, 128, 140_000  # 32 KiB of codes a page: 4.6e9 bytes
+    P = nv()
+    big = (*(torch.empty(n, H, 64, dh // 2, dtype=torch.uint8, device="cuda") for _ in "kv"),
+           *(torch.empty(n, H, 64, dh // 32, dtype=torch.uint8, device="cuda") for _ in "kv"))
+    small = P.nv_kv4_pages(6, H, dh, "cuda")
+    ids = np.array([[n - 1, 5, n - 2], [131_072, 131_071, n - 3]])
+    tb, ts = i32(ids), i32(np.arange(6).reshape(2, 3))
+    k, v = rand(1, 2, 190, H * dh, dtype=F16), rand(2, 2, 190, H * dh, dtype=F16)
+    pos = i32([0, 0])
+    for d, t in ((big, tb), (small, ts)):
+        P.nv_op_kv4_append(k, v, d, t, pos)
+    for a, b in zip(P.nv_op_kv4_read(big, tb, pos, 190), P.nv_op_kv4_read(small, ts, pos, 190)):
+        assert torch.equal(a, b)
+    want, _ = O.quantise(np64(k).reshape(2, 190, H, dh))
+    assert np.array_equal(big[0][n - 1, :, 7].cpu().numpy(), want[0, 7])
+    for S in (1, 300):
+        q = rand(3, 2, S, 2 * H * dh, dtype=F16)
+        for lens in ([190, 180], [7, 100]):
+            assert torch.equal(P.nv_op_attention_kv4(q, big, tb, i32(lens), 0.1),
+                               P.nv_op_attention_kv4(q, small, ts, i32(lens), 0.1))
+
+
 def test_read_into_views_and_of_any_byte():
     """Rows inside a larger buffer, unaligned ones; every code with every scale."""
     pages = pages_np(9, 5, 2, 40)
