@@ -67,8 +67,9 @@ __global__ void __launch_bounds__(256) kv4_append_k(Kv4AppendArgs a) {
 // -------------------------------------------------------------------------------------- read
 
 // Units of eight channels from which on a lane takes two at once: their way from a position over the
-// table to the tokens is waited for once.
-constexpr int64_t READ_TWO = 1 << 19;
+// table to the tokens is waited for once (8 rows of 8 heads of 128, one unit and two: 512 tokens, 2^19 units,
+// 5.4 and 5.6 us; 1024, 8.7 and 8.8; 2048, 14.9 and 14.8; 4096, 38 and 34 with outputs in turn).
+constexpr int64_t READ_TWO = 1 << 21;
 
 // Eight channels of a token's keys and values a lane, N times; a token's heads one after another, as the
 // output has them.  Bound by HBM's writes: 8 x 4096 tokens of 8 heads of 128 (134 MB out) 34 us with operands
