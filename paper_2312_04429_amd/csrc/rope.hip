@@ -232,12 +232,14 @@ extern "C" int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_strid
   a.norm = norm, a.eps = eps, a.tokens = (int64_t)rows * S;
   int group = 1;
   while (group * 8 < dh) group *= 2;
-  // Few tokens: a step a wave, as many workgroups as that takes; many: about ten steps a wave, which pay
-  // for the tokens' angles and the workgroup's start.
-  const int64_t all = ceil_div(heads, 64 / group);
-  const bool few = a.tokens * all <= 4 * 2048;
-  const int tt = few ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, 40 / all));
-  const int steps = few ? 4 : (int)all;
+  // About ten steps a wave pay for the tokens' angles and the workgroup's start, but a step is 1 us of
+  // latency: tokens share a workgroup only where there are 1024 workgroups without, and where there are
+  // not 512 the heads are dealt out too (40 heads of 64, ten steps always: 256 tokens 9.4 us, 1024 10.1, 8192
+  // 20.0; a step always: 4.4, 10.2 and 62; so: 4.3, 7.3 and 20.3; tokens shared from 4096 on: 22.7).
+  const int64_t all = ceil_div(heads, 64 / group), least = std::max<int64_t>(1, 4 / all);
+  const int tt = (int)std::max(least, std::min<int64_t>({16, 40 / all, a.tokens / 1024}));
+  const int64_t parts = std::min(ceil_div(all, 4), ceil_div(512, ceil_div(a.tokens, tt)));
+  const int steps = (int)ceil_div(all, parts);
   const int64_t wgs = ceil_div(a.tokens, tt);
   if (wgs > 8388607) {
     set_error("more tokens than a grid holds");
