@@ -636,7 +636,7 @@ int32_t nv_op_attention_kv8(const void* q, int64_t ldq, int64_t q_row_stride, in
  *   dh a multiple of 8, 8 <= dh <= 256 (NV_ERR_UNSUPPORTED otherwise); strides of
  *   any size (multiples of 8 with 16-byte aligned buffers are fastest), an
  *   output's ld >= heads * dh.  An output may be its input with the same strides.
- *   At most 2^20 heads and 2^23 - 1 tokens (beyond: NV_ERR_UNSUPPORTED).
+ *   At most 2^20 heads; more than 2^23 - 1 tokens may be refused (NV_ERR_UNSUPPORTED).
  * ------------------------------------------------------------------------ */
 int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_stride, void* q_out, int64_t ldqo,
                       int64_t qo_row_stride, int32_t q_heads, const float* q_weight, const void* k,

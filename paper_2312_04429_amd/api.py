@@ -801,6 +801,7 @@ def _attention(q, cache, table, lens, scale, qpos, out, ws, name):
 
 _F64 = (torch.float64,)
 _CODES4 = frozenset((torch.float4_e2m1fn_x2, torch.uint8))
+_INTS = tuple(C.c_int32 * n for n in range(8))
 
 
 def nv_rope_freqs(axes, theta=10000.0, device="cuda"):
@@ -857,7 +858,7 @@ def nv_op_qk_rope(q, k, dh, pos, axes, freqs, q_weight=None, k_weight=None, eps=
     _call("nv_op_qk_rope", dev, q.data_ptr(), ldq, qr, qo.data_ptr(), ldqo, qor, cols // dh,
           _at(q_weight), _at(k), ldk, kr, _at(ko), ldko, kor, kcols // dh, _at(k_weight),
           _DT[q.dtype], rows, S, dh, pos.data_ptr(), ps[1], ps[0], n,
-          (C.c_int32 * n)(*axes), freqs.data_ptr(), halves, eps is not None,
+          _INTS[n](*axes) if n < 8 else (C.c_int32 * n)(*axes), freqs.data_ptr(), halves, eps is not None,
           0.0 if eps is None else eps)
     return qo, ko
 
@@ -874,13 +875,18 @@ def nv_kv4_pages(n_pages, heads, dh, device):
 def _pages4(pages, dev):
     """Checks a 4-bit cache and returns (kp, vp, ks, vs, n_pages, heads, dh)."""
     kp, vp, ks, vs = pages
-    if kp.dim() != 4 or kp.shape[2] != N.NV_KV4_PAGE:
+    codes, scales = kp.shape, ks.shape
+    if len(codes) != 4 or codes[2] != N.NV_KV4_PAGE:
         raise ValueError("kp must be [n_pages][heads][64][dh / 2]")
-    n, h, _, b = kp.shape
-    _want(kp, "kp", _CODES4, dev, None, True)
-    _want(vp, "vp", _CODES4, dev, kp.shape, True)
-    _want(ks, "ks", _SCALES, dev, (n, h, N.NV_KV4_PAGE, -(-b // 16)), True)
-    _want(vs, "vs", _SCALES, dev, ks.shape, True)
+    n, h, _, b = codes
+    if not (scales == (n, h, N.NV_KV4_PAGE, -(-b // 16)) and vp.shape == codes and vs.shape == scales and
+            kp.get_device() == vp.get_device() == ks.get_device() == vs.get_device() == dev and
+            kp.dtype in _CODES4 and vp.dtype in _CODES4 and ks.dtype in _SCALES and vs.dtype in _SCALES and
+            kp.is_contiguous() and vp.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+        _want(kp, "kp", _CODES4, dev, None, True)  # says which
+        _want(vp, "vp", _CODES4, dev, codes, True)
+        _want(ks, "ks", _SCALES, dev, (n, h, N.NV_KV4_PAGE, -(-b // 16)), True)
+        _want(vs, "vs", _SCALES, dev, ks.shape, True)
     return kp, vp, ks, vs, n, h, 2 * b
 
 
