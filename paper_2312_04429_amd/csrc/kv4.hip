@@ -149,6 +149,7 @@ constexpr float P_TOP = 15.f;
 // The reference under which a score of `top` has the probability 2^room (room <= P_TOP): top - room, or
 // top itself where the scores are so large that this rounds to more than P_TOP below it.
 __device__ __forceinline__ float reference(float top, float room) {
+#pragma clang fp contract(off)  // top is a rounded product, and has to be the same one in both lines
   const float low = top - room;
   return top - low > P_TOP ? top : low;
 }
@@ -446,8 +447,17 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>
         top = fmaxf(top, s[t][r]);
       }
   }
-  const float mnew = fmaxf(st.m, reference(rows_max(top) * scale2, P_TOP)),
-              base = mnew == -INFINITY ? 0.f : mnew;
+  // Scores are multiplied by the scale inside the exponent, where the product is not rounded; the reference
+  // comes from a rounded one.  From 2^23 on the two differ by 1/2 and more (2^29: by 32, past float16 either
+  // way), so there scores are rounded first: 2^23 leaves the largest probability 2^(P_TOP + 1/4).
+  const float largest = rows_max(top * scale2), size = fabsf(largest);
+  float rest = scale2;
+  if (__ballot(size >= 0x1p23f && size < INFINITY)) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] *= scale2;
+    rest = 1.f;
+  }
+  const float mnew = fmaxf(st.m, reference(largest, P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
   if (__ballot(mnew != st.m)) {
     const float alpha = __builtin_amdgcn_exp2f(st.m - base);
 #pragma unroll
@@ -460,7 +470,7 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[t][r], scale2, -base));
+      fp[t >> 1][(t & 1) * 4 + r] = (_Float16)__builtin_amdgcn_exp2f(fmaf(s[t][r], rest, -base));
   st.l += add_probs(fp, floatx4{0.f, 0.f, 0.f, 0.f})[0];
 #pragma unroll
   for (int j = 0; j < D::DV; ++j)
