@@ -686,8 +686,9 @@ int32_t nv_op_qk_rope(const void* q, int64_t ldq, int64_t q_row_stride, void* q_
  *   keys their whole result, one of values its 32 channels.  float32 scores, softmax
  *   and sums; the probabilities enter the second product rounded to 2^-11 of
  *   themselves or 2^-34 of the query's largest, and the same rounded ones make the
- *   sum it is divided by.  Values of 2^90 and more may overflow the sums, keys and
- *   values below 2^-126 may count as zero.  scale finite.
+ *   sum it is divided by.  Keys and values of 2^90 and more may overflow the sums of
+ *   queries that see them; keys and values below 2^-126 may count as zero, and values below
+ *   2^-122 in a page with a value scale of 253 or 254.  scale finite.
  *   workspace: device, >= nv_op_attention_kv4_workspace(...) bytes (0: may be
  *   NULL), 256-byte aligned, contents need not be initialised. */
 #define NV_KV4_PAGE 64

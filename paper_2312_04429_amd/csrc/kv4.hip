@@ -214,19 +214,31 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
   const float mnew = fmaxf(st.m, reference(rows_max(top), P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
   const float alpha = __builtin_amdgcn_exp2f(st.m - base);
   st.m = mnew;
+  // The larger codes of scales 253 and 254 are 2^128 and more, infinite in bfloat16, and would reach queries
+  // that do not see their token (0 * infinity): with such a scale the page's values count as eighths,
+  // its probabilities eightfold.
+  bool wide = false;
+#pragma unroll
+  for (int b = 0; b < D::NB; ++b) {
+    const int tok = 16 * kc + li;
+    wide |= j0 + tok < len && (unsigned)(vs[tok * D::NB + b] - 253) <= 1u;
+  }
+  const bool eighths = __ballot(wide);
+  const int less = eighths ? 3 : 0;
+  const float times = eighths ? 8.f : 1.f;
   float sum = 0.f;
   bf16x8 ph8[2], pl8[2];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float p = __builtin_amdgcn_exp2f(s[t][r] - base);
+      const float p = __builtin_amdgcn_exp2f(s[t][r] - base) * times;
       __bf16 hi, lo;
       split_bf16(p, &hi, &lo);
       ph8[t >> 1][(t & 1) * 4 + r] = hi, pl8[t >> 1][(t & 1) * 4 + r] = lo;
       sum += (float)hi + (float)lo;
     }
-  st.l = st.l * alpha + rows_sum(sum);
+  st.l = st.l * alpha + rows_sum(sum) / times;
   float nan[D::NB];
 #pragma unroll
   for (int b = 0; b < D::NB; ++b) {
@@ -253,10 +265,10 @@ __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>:
         const int tok = 32 * h + 4 * kc + (i < 4 ? i : i + 12);
         v[i] = (__bf16)0.f;
         if (j0 + tok < len && c < DH) {
-          const int e = vs[tok * D::NB + c / KV4_BLOCK];
+          const int e = vs[tok * D::NB + c / KV4_BLOCK] - less;
           const uint32_t w = vp[(tok * DH + c) / 2];
           const bf16x2 two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_value(e), 0);
-          if (e != 255) v[i] = two[c & 1];
+          if ((unsigned)e < 255u - less) v[i] = two[c & 1];
         }
       }
       st.acc[j] = B::mul(v, ph8[h], st.acc[j]);

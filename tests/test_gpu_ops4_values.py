@@ -1,5 +1,5 @@
-"""Attention over the 4-bit cache where scores are far from one another in size, against the value that the
-definition picks."""
+"""Attention over the 4-bit cache where scores or values are far from one another in size, against what the
+definition gives."""
 import numpy as np
 import pytest
 import torch
@@ -63,3 +63,74 @@ def test_scores_of_any_size_pick_the_largest(rows, S, W, sign, way):
             for m in (1.0, 1.13, 1.37, 1.71):
                 got = run(q, (kp, vp, ks, vs), table, [W * 64], sign * m * 2.0 ** e / 384, rows=rows)
                 assert (got == want).all(), (at, e, m, got[0, :8].tolist(), want[:8].tolist())
+
+
+# ------------------------------------------------------------------- values that bfloat16 does not hold
+
+def cache(seed, W, H=1, dh=64):
+    """Ordinary keys and values: [kp, vp, ks, vs], table [1][W]."""
+    rng = np.random.default_rng(seed)
+    (kp, ks), (vp, vs) = (O.quantise(rng.standard_normal((W, H, 64, dh))) for _ in "kv")
+    return [kp, vp, ks, vs], rng.permutation(W).reshape(1, W).astype(np.int32)
+
+
+def fill(pages, table, at, scale):
+    """Every code under the scale bytes `scale` in the tokens `at` of the row: keys and values."""
+    pages = [p.copy() for p in pages]
+    for t in at:
+        for i in (0, 1):
+            pages[i][table[0, t // 64], :, t % 64] = np.arange(t, t + pages[i].shape[3]) * 7 % 256
+            pages[i + 2][table[0, t // 64], :, t % 64] = scale
+    return pages
+
+
+def same(a, b):
+    return torch.equal(a.contiguous().view(torch.int16), b.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rows,S,W", PLANS)
+def test_largest_scales_behind_the_limit_leave_a_query_alone(rows, S, W, dtype):
+    """Tokens before a row's last one that no query sees, or only the last half of them, of scales whose larger
+    codes are infinite in bfloat16: the others' results are the bits of a call that has 2^23 there."""
+    n = W * 64
+    pages, table = cache(W, W)
+    q = torch.randn(S, 64, generator=torch.Generator().manual_seed(S)).to(dtype).cuda()
+    for last in (n - 30, n - 64, n - 130 if S < 130 else n - 1):       # tokens that the last query sees
+        half = S // 2
+        for seen, at in ((S, range(last, n)), (half, range(last - S + half, n))):
+            want = run(q, fill(pages, table, at, 150), table, [n], 0.125, [last - S], rows)
+            o = O.attention(q.double().cpu().numpy()[None, :, None], *pages, table, [n], 0.125, 1, [last - S])[0]
+            assert np.abs(want.double().cpu().numpy()[:seen] - o[0, :seen, 0]).max(initial=0) < 0.02
+            for e in (253, 254, 255):
+                print("attention_kv4 behind", rows, S, W, dtype, last, seen, e, flush=True)
+                got = run(q, fill(pages, table, at, e), table, [n], 0.125, [last - S], rows)
+                assert same(got[:seen], want[:seen])
+
+
+@pytest.mark.parametrize("rows,S,W", PLANS)
+def test_largest_bfloat16_values(rows, S, W):
+    """bfloat16's largest numbers, appended: 2^128 as 4 bits have them.  Queries before them are as without,
+    in the same block too; no result behind them is a number that is not near 2^128 times its share.  (Infinite
+    or NaN it may be: a probability is up to 2^15 as two numbers of either sign, and both products pass
+    2^128.)"""
+    P, n = nv(), W * 64
+    x = torch.randn(2, 1, n, 64, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    q = torch.randn(S, 64, generator=torch.Generator().manual_seed(2)).to(BF16).cuda()
+    table = dev(np.random.default_rng(3).permutation(W).reshape(1, W).astype(np.int32))
+    first, big = n - S // 2 - 5, torch.finfo(BF16).max
+    outs = []
+    for value in (2.0 ** 20, big):
+        x[1, 0, first, 7] = value
+        x[1, 0, first, 40] = -value
+        d = P.nv_kv4_pages(W, 1, 64, "cuda")
+        P.nv_op_kv4_append(x[0], x[1], d, table, dev(np.zeros(1, np.int32)))
+        d = tuple(t.view(torch.uint8).cpu().numpy() for t in d)
+        outs.append(run(q, d, table.cpu().numpy(), [n], 0.125, [n - S], rows))
+    before = max(0, first - n + S)                                       # queries that end before it
+    assert same(outs[0][:before], outs[1][:before]) and outs[0].isfinite().all()
+    for c, sign in ((7, 1), (40, -1)):
+        behind = sign * outs[1][before:, c].double().cpu()
+        share = outs[0][before:, c].abs().double().cpu() / 2.0 ** 20     # of the token, about
+        near = behind / 2.0 ** 128 / share
+        assert near.numel() and ((near > 0.9) & (near < 1.1) | ~behind.isfinite()).all(), near
