@@ -459,24 +459,27 @@ __device__ __forceinline__ void page_step(State<DH>& st, const typename Half8<T>
         top = fmaxf(top, s[t][r]);
       }
   }
-  // Scores are multiplied by the scale inside the exponent, where the product is not rounded; the reference
-  // comes from a rounded one.  From 2^23 on the two differ by 1/2 and more (2^29: by 32, past float16 either
-  // way), so there scores are rounded first: 2^23 leaves the largest probability 2^(P_TOP + 1/4).
-  const float largest = rows_max(top * scale2), size = fabsf(largest);
+  // Scores are multiplied by the scale inside the exponent, where the product is not rounded, and measured
+  // against the reference in the same way.  It moves only when a probability would pass 2^P_TOP.  A new one
+  // comes from rounded products: from 2^23 on those differ by 1/2 and more from the others (2^29: by 32, past
+  // float16 either way), so this page's scores are rounded, too (below, the largest probability is 2^(P_TOP +
+  // 1/4)); a later page's that pass P_TOP without being rounded come back here.
   float rest = scale2;
-  if (__ballot(size >= 0x1p23f && size < INFINITY)) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] *= scale2;
-    rest = 1.f;
-  }
-  const float mnew = fmaxf(st.m, reference(largest, P_TOP)), base = mnew == -INFINITY ? 0.f : mnew;
-  if (__ballot(mnew != st.m)) {
-    const float alpha = __builtin_amdgcn_exp2f(st.m - base);
+  if (__ballot(fmaf(rows_max(top), scale2, -st.m) > P_TOP)) {  // at the start: infinite
+    const float largest = rows_max(top * scale2), size = fabsf(largest);
+    const float mnew = fmaxf(st.m, reference(largest, P_TOP));
+    const float alpha = __builtin_amdgcn_exp2f(st.m - (mnew == -INFINITY ? 0.f : mnew));
 #pragma unroll
     for (int j = 0; j < D::DV; ++j) st.acc[j] *= alpha;
     st.l *= alpha;
     st.m = mnew;
+    if (__ballot(size >= 0x1p23f && size < INFINITY)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t] *= scale2;
+      rest = 1.f;
+    }
   }
+  const float base = st.m == -INFINITY ? 0.f : st.m;
   half8 fp[2];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
