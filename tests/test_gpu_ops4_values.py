@@ -134,3 +134,76 @@ def test_largest_bfloat16_values(rows, S, W):
         share = outs[0][before:, c].abs().double().cpu() / 2.0 ** 20     # of the token, about
         near = behind / 2.0 ** 128 / share
         assert near.numel() and ((near > 0.9) & (near < 1.1) | ~behind.isfinite()).all(), near
+
+
+# ------------------------------------------------------------------------------- scales far apart
+
+def bound(q, pages, table, n, scale, first, dtype):
+    """(o, tol) [S][G][dh] of q [1][S][G][dh] over one row: a score is dh float32 additions and three products,
+    the exponential 4 E |score| + 4 E, twice that for a probability (numerator and sum); its rounding 2^-11 of
+    itself or 2^-34 of the query's largest where it is small, and then of the largest value of the channel
+    that THIS query sees; n E for sums of n terms; one rounding of the result."""
+    E, dh = 2.0 ** -23, q.shape[3]
+    o, spread, size, most = O.attention(q, *pages, table, [n], scale, 1, [first])
+    v = np.abs(O.row_of(pages[1], pages[3], table[0], n, 0)[0])
+    last = np.clip(first + np.arange(q.shape[1]), -1, n - 1)
+    seen = np.where(last[:, None] < 0, 0, np.maximum.accumulate(v)[last])[:, None]
+    rel = 2 * (dh * E * size + 8 * E * most + 4 * E) + 2.0 ** -10 + n * E
+    half = torch.finfo(dtype).eps / 2
+    tol = rel * spread * (1 + half) + n * 2.0 ** -34 * (seen + np.abs(o)) + half * np.abs(o) \
+        + (2.0 ** -25 if dtype == F16 else 0)
+    return o[0], tol[0]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("S,G,N", [(9, 1, 1), (40, 1, 1), (300, 1, 1), (70, 4, 1), (120, 4, 96)])
+def test_scales_far_apart_under_a_limit(S, G, N, dtype):
+    """Values far above a query's own behind its limit leave its result as exact as without them, and values far
+    below the largest keep their bits where only they are seen."""
+    for dh in (64, 128):
+        n, rng = 320, np.random.default_rng(S)
+        for lo, hi in ((90, 138), (1, 120), (120, 130), (20, 160 if dtype == BF16 else 136)):
+            pages, table = cache(2, 5, dh=dh)
+            pages[3][:] = np.where(rng.random(pages[3].shape) < 0.02, lo, 126)
+            pages[3][table[0, 1]] = lo
+            pages[3][table[0, 3], :, 20:23] = hi        # tokens 212 to 214
+            pages[3][table[0, 2], :, 7] = lo
+            pages[3][table[0, 4], :, 8, -1] = hi
+            if dtype == F16:                             # results within the type
+                pages[1][table[0, 3], :, 20:23] &= 0x99
+                pages[1][table[0, 4], :, 8] &= 0x99
+            q = torch.randn(S, G * dh, generator=torch.Generator().manual_seed(S)).to(dtype).cuda()
+            q64 = q.double().cpu().numpy().reshape(1, S, G, dh)
+            for first in (n - S, 200 - S // 2, 211 - S):
+                print("attention_kv4 far", S, G, N, dtype, dh, lo, hi, first, flush=True)
+                got = run(q, pages, table, [n], dh ** -0.5, [first], N).double().cpu().numpy()
+                o, tol = bound(q64, pages, table, n, dh ** -0.5, first, dtype)
+                bad = ~(np.abs(got.reshape(o.shape) - o) <= tol)
+                assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("dh", [16, 32, 40, 64, 80, 128, 160])
+def test_large_scores_of_any_head(dh, dtype):
+    """The largest of scores of 2^23 to 2^38 under tiles of 16, 64 and 128, in ordinary pages and in pages that
+    16 bits do not hold."""
+    W, rng = 6, np.random.default_rng(dh)
+    table = rng.permutation(W).reshape(1, W).astype(np.int32)
+    nb = -(-dh // 32)
+    for rows, S in ((1, 3), (1, 300), (300, 300)):
+        print("attention_kv4 large scores", rows, S, dh, dtype, flush=True)
+        q = torch.zeros(S, dh, dtype=dtype, device="cuda")
+        q[:, dh - 1] = 1 + torch.arange(S, device="cuda") % 61 / 64
+        for at, way in ((70, 0), (W * 64 - 1, 0), (130, 1)):
+            page, slot = table[0, at // 64], at % 64
+            kp = np.zeros((W, 1, 64, dh // 2), np.uint8)
+            kp[..., -1] = rng.integers(4, 7, (W, 1, 64)) << 4
+            kp[page, 0, slot, -1] = 7 << 4
+            vp = rng.integers(0, 256, (W, 1, 64, dh // 2)).astype(np.uint8)
+            ks, vs = np.full((W, 1, 64, nb), 133, np.uint8), np.full((W, 1, 64, nb), 127, np.uint8)
+            if way:
+                vp[page, 0, slot ^ 1, 0], vs[page, 0, slot ^ 1, 0] = 0x77, 150
+            want = dev(O.values(vp[page, 0, slot], vs[page, 0, slot])).to(dtype)
+            for e in range(23, 39):
+                got = run(q, (kp, vp, ks, vs), table, [W * 64], 1.37 * 2.0 ** e / 384, rows=rows)
+                assert (got == want).all(), (at, e)
