@@ -44,11 +44,14 @@ inline double kv4_cost(double rh, int64_t cols, int dh, int table_w, int tall, i
 }
 
 // The cheapest of the three tiles and of 1, 2, 4 .. shares of at least four pages each, by the cost
-// above.  Of 98 sizes (1 to 8192 queries a kv head, 2 to 512 heads, 2 to 1024 pages, 64 and 128 channels)
-// it takes 1.5 % more than the best measured choice on average, 15 % at most (one query over 65536 tokens of
-// 8 heads of 128: 345 us in one piece, 32 in 16 shares, 23 in 64; 256 queries over 4096: 20.3 in tiles of 16
-// with four shares, 22.8 in tiles of 64 with eight, 26 of 128 with sixteen).  Shares stay within 1024
-// workgroups, and so do the partial results (84 MB).
+// above.  Of 98 sizes (1 to 8192 queries a kv head, 2 to 1024 heads, 2 to 1024 pages, 64 and 128 channels,
+// full rows) it takes 1.5 % more than the best measured choice on average, 15 % at most (one query over 65536
+// tokens of 8 heads of 128: 345 us in one piece, 32 in 16 shares, 23 in 64; 256 queries over 4096: 20.3 in
+// tiles of 16 with four shares, 22.8 in tiles of 64 with eight, 26 of 128 with sixteen).  Of 56 sizes of 32, 40,
+// 80 and 160 channels, which it was not fitted to, 0.9 and 8 %; of 14 of 16 channels 4.5 %, 11 % at most but for
+// one of 39 % (2 rows of 8 heads, 96 queries a head, 64 pages: 16.9 us in one piece, 12.2 in four shares).  A
+// causal limit is not priced: every tile counts as the longest.  Shares stay within 1024 workgroups, and so do
+// the partial results (84 MB).
 inline Kv8Plan kv4_plan(int64_t rows, int S, int heads, int kv_heads, int dh, int table_w) {
   // products of three sizes are taken in float64: they may pass 64 bits before they are refused
   const int64_t cols = (int64_t)S * (heads / kv_heads);

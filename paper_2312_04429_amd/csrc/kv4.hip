@@ -143,7 +143,10 @@ struct State {
   floatx4 acc[Dims<DH>::DV];
 };
 
-// The largest probability is at most 2^P_TOP, which float16 holds.
+// Probabilities enter the second product in float16: 2^-11 of themselves is lost, of those that the sum is made
+// of too, so that a mean stays one.  One query over 200000 tokens, float16: 2.8e-4 from float64 where a result
+// rounded once is 2.1e-4; as sums of two float16 numbers 2.1e-4, for 2 to 10 % of the time.  With
+// bfloat16 results it does not show.  The largest probability is at most 2^P_TOP, which float16 holds.
 constexpr float P_TOP = 15.f;
 
 // The reference under which a score of `top` has the probability 2^room (room <= P_TOP): top - room, or
@@ -165,6 +168,8 @@ __device__ __forceinline__ void split_bf16(float x, __bf16* hi, __bf16* lo) {
 // every scale; float16 queries, and probabilities, as sums of two.  Everything comes from global memory
 // as it is needed.  j0: the page's first token; lim: tokens this lane's query sees; len: tokens of
 // the sequence.  A NaN block of values reaches the queries that see its token, in its 32 channels.
+// Written for few registers, not speed: where every page goes this way one query over 200000 tokens takes
+// 498 us for 43, 2 x 2048 queries over 4096 3900 for 140; with one such page a row 77 and 303.
 template <typename T, int DH, bool NEAR>
 __device__ __forceinline__ void page_any(State<DH>& st, const typename Half8<T>::Vec* fq,
                                          const Kv4AttnArgs& a, int64_t ph, float scale2, int j0,
@@ -656,8 +661,9 @@ __global__ void __launch_bounds__(NW * 64, 2) attn_kv4_tall_k(Kv4AttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rh = blockIdx.x % (a.rows * a.kv_heads);  // a multiple of 8: one XCD's L2 for a head
   const int rest = blockIdx.x / (a.rows * a.kv_heads), split = rest / a.col_tiles;
-  // Longest first, where not all are resident at once; where they are, a compute unit's second workgroup
-  // is as short as its first is long (a causal limit from 2048 of 4096 tokens: 126 -> 117 us).
+  // Longest first, where not all are resident at once (two a compute unit; one past 128 channels, where the
+  // pairing below is without effect); where they are, a compute unit's second workgroup is as short as its
+  // first is long (a causal limit from 2048 of 4096 tokens: 126 -> 117 us).
   const int nth = rest % a.col_tiles, half = (a.col_tiles + 1) / 2;
   const int ct = nth < half || gridDim.x > 512 ? a.col_tiles - 1 - nth : nth - half;
   const int head = rh % a.kv_heads, row = rh / a.kv_heads;

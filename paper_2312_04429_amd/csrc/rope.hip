@@ -54,6 +54,8 @@ __device__ __forceinline__ float group_sum(float v) {
 // 64-bit division by S a lane and step, 16384 tokens of 40 heads of 128 took 158 us).  Bound by HBM: those
 // tokens, bfloat16, three axes: 335 MB in 78 us (4.3 TB/s); 8346 tokens of 40 heads of 64, float16: 22 us
 // (3.8); 32 single tokens of 40 heads of 128: 4.9 us, launch and the way from a position to its angles.
+// Halves cost their way through LDS: 16384 tokens of 40 heads of 128, bfloat16, NEXT 77 us, HALF8 92, HALF 87; 4096
+// tokens 24, 31 and 27; 8346 of 64 channels 22, 28 and 27.
 template <typename T, int GROUP, Pairs P, bool VEC>
 __global__ void __launch_bounds__(256) qk_rope_k(RopeArgs a, int tt, int steps) {
   constexpr int HPW = 64 / GROUP;  // heads of a step
